@@ -204,6 +204,114 @@ int s2o_attention_prefix(const void* Q, const void* K, const void* V, const s2o_
                          int32_t* computed, int32_t* skipped, const void* scratch, size_t scratch_bytes,
                          void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * The cache behind a prefill: s2o_decode attends it, s2o_key_weights says what each of its keys was
+ * worth, s2o_evict cuts it down to the best ones.  The conventions above hold, with these differences:
+ *   - elements are bf16 or fp16 (`dtype`), head_dim is 64 or 128, lengths need not be multiples of anything;
+ *   - strides of dimensions of size 1 are not looked at; a K, V row stride is less than 16 MiB, a head may span any
+ *     number of bytes;
+ *   - `lens` arrays (int32, device) say how many rows of a cache are filled; NULL: all that `cache_len` (`own_len`) counts.
+ *     They are read by the kernels, so a captured call follows them; values outside [0, cache_len] are clamped.
+ *     Rows behind them are never read into a result, whatever they hold;
+ *   - the calls can be captured from the first one on (they set no kernel attributes). */
+enum { S2O_BF16 = 0, S2O_F16 = 1 };
+
+typedef struct s2o_decode_params {
+  int32_t struct_size;   /* = sizeof(s2o_decode_params)                                    */
+  int32_t batch;         /* Z: shared caches                                               */
+  int32_t branches;      /* B: sequences that continue each of them                        */
+  int32_t q_heads;       /* H                                                              */
+  int32_t kv_heads;      /* Hkv, H % Hkv == 0                                              */
+  int32_t head_dim;      /* D: 64 or 128                                                   */
+  int32_t q_len;         /* T: query tokens of a sequence, the last T of its own rows      */
+  int32_t cache_len;     /* L: rows a shared cache has memory for; 0: there is none        */
+  int32_t own_len;       /* Lo: rows a sequence's own cache has memory for; 0: there is none */
+  int32_t dtype;         /* S2O_BF16 or S2O_F16: of Q, K, V and O                          */
+  float softmax_scale;   /* 0 -> 1/sqrt(D)                                                 */
+  int32_t reserved;      /* 0                                                              */
+  int64_t q_stride[4];   /* element strides of Q for (z, b, h, t); all 0 -> packed [Z,B,H,T,D] */
+  int64_t k_stride[3];   /* (z, h, l) of the shared K, [Z,Hkv,L,D]                         */
+  int64_t v_stride[3];
+  int64_t own_k_stride[4]; /* (z, b, h, l) of the sequences' own K, [Z,B,Hkv,Lo,D]         */
+  int64_t own_v_stride[4];
+  int64_t o_stride[4];   /* like q_stride; rows of O must not overlap                      */
+} s2o_decode_params;
+
+/* Sizes of lse and of the scratch buffer (0: none is needed; any out-pointer may be NULL). */
+int s2o_decode_sizes(const s2o_decode_params* params, size_t* lse_bytes, size_t* scratch_bytes);
+
+/* Attention of B sequences that share a cache (their common prompt, read once for all of them), each with
+ * rows of its own behind it.  Query t of sequence (z, b) sees the shared rows j < lens[z] and of its own p = own_lens[z*B+b]
+ * rows those with j <= p - T + t:
+ *   O = sum_j exp(x_j - lse) v_j,  x_j = scale <q, k_j>,  lse = log sum_j exp(x_j)   (natural logarithm)
+ * A query that sees nothing gets O = 0 and lse = -infinity.  An infinity or NaN in a row that a query does not see does not
+ * reach it.
+ *   lens      [Z] or NULL; own_lens [Z,B] or NULL
+ *   O         [Z,B,H,T,D];  lse  [Z,B,H,T] fp32, packed, or NULL
+ *   scratch   device, 256-byte aligned, of at least the size s2o_decode_sizes reports; contents undefined afterwards.
+ * The result has the same bits every time for the same arguments. */
+int s2o_decode(const void* Q, const void* K, const void* V, const void* own_K, const void* own_V, const int32_t* lens,
+               const int32_t* own_lens, const s2o_decode_params* params, void* O, float* lse, void* scratch, size_t scratch_bytes,
+               void* stream);
+
+typedef struct s2o_weights_params {
+  int32_t struct_size;   /* = sizeof(s2o_weights_params)                                   */
+  int32_t batch, branches, q_heads, kv_heads, head_dim, q_len;   /* Z, B, H, Hkv, D, T as above */
+  int32_t cache_len;     /* L: rows a cache has memory for, at least 1                     */
+  int32_t dtype;         /* S2O_BF16 or S2O_F16: of Q and K                                */
+  int32_t causal;        /* 0: every query sees the whole cache.  1: the queries belong to the cache's last T
+                            rows: query t sees the rows j <= lens[z] - T + t               */
+  float softmax_scale;   /* 0 -> 1/sqrt(D)                                                 */
+  int32_t reserved;      /* 0                                                              */
+  int64_t q_stride[4];   /* (z, b, h, t) of Q [Z,B,H,T,D]; all 0 -> packed                 */
+  int64_t k_stride[3];   /* (z, h, l) of K [Z,Hkv,L,D]                                     */
+} s2o_weights_params;
+
+/* Size of the scratch buffer of a call with / without `lse`; the first argument says which (0: without). */
+int s2o_key_weights_sizes(const s2o_weights_params* params, int with_lse, size_t* weights_bytes, size_t* scratch_bytes);
+
+/* Accumulated attention weights of a cache's keys:
+ *   weights[z,g,j] = prev[z,g,j] + sum over b, the query heads h of KV head g, and the t that see row j
+ *                    of exp(scale <q_bht, k_j> - lse[z,b,h,t])
+ *   lse       [Z,B,H,T] fp32, the queries' log-sum-exp (as s2o_decode leaves it, over more than these keys perhaps); queries with an
+ *             infinite one add nothing.  NULL: that of the keys the query sees here.
+ *   lens      [Z] or NULL
+ *   prev      [Z,Hkv,L] fp32 or NULL (0).  It may be `weights` itself, but must not overlap it otherwise.
+ *   weights   [Z,Hkv,L] fp32; entries j >= lens[z] are left as they were.
+ *   scratch   as above; NULL where the size is 0.
+ * Sums are held in fp32 and made in one order: the same bits every time for the same arguments. */
+int s2o_key_weights(const void* Q, const void* K, const float* lse, const int32_t* lens, const s2o_weights_params* params, const float* prev,
+                    float* weights, void* scratch, size_t scratch_bytes, void* stream);
+
+typedef struct s2o_evict_params {
+  int32_t struct_size;   /* = sizeof(s2o_evict_params)                                     */
+  int32_t batch, kv_heads, head_dim;   /* Z, Hkv, D                                        */
+  int32_t cache_len;     /* L: rows a cache has memory for, at least 1                     */
+  int32_t keep;          /* rows that stay, 1 <= keep <= L                                 */
+  int32_t sink, recent;  /* the first and the last rows that stay whatever their weight, sink + recent <= keep */
+  int32_t dtype;         /* S2O_BF16 or S2O_F16 (rows are moved, not computed with)        */
+  int32_t reserved;      /* 0                                                              */
+  int64_t k_stride[3];   /* (z, h, l) of K [Z,Hkv,L,D]; all 0 -> packed                    */
+  int64_t v_stride[3];
+  int64_t out_k_stride[3]; /* of K_out [Z,Hkv,keep,D]; rows must not overlap               */
+  int64_t out_v_stride[3];
+} s2o_evict_params;
+
+/* Size of the scratch buffer of s2o_evict (may be 0). */
+int s2o_evict_sizes(const s2o_evict_params* params, size_t* scratch_bytes);
+
+/* Cuts a cache down: of its n = lens[z] rows, m = min(n, keep) stay: the first `sink`, the last `recent`, and of the others those with the
+ * largest weights (equal ones: the lowest index; -0 and +0 are equal; NaN counts as -infinity).  They are moved together in the
+ * order they had:
+ *   kept        [Z,Hkv,keep] int32: their indices, ascending
+ *   K_out,V_out [Z,Hkv,keep,D]: their rows (K and K_out, or V and V_out, may both be NULL: nothing is moved)
+ *   weights_out [Z,Hkv,keep] fp32: their weights, or NULL
+ *   lens_out    [Z] int32: m, or NULL
+ * Entries behind m are left as they were.  The outputs must not overlap the inputs or each other (S2O_EINVAL where the ranges that they
+ * span do).  scratch as above. */
+int s2o_evict(const void* K, const void* V, const float* weights, const int32_t* lens, const s2o_evict_params* params, void* K_out,
+              void* V_out, float* weights_out, int32_t* kept, int32_t* lens_out, void* scratch, size_t scratch_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

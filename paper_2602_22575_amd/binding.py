@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from functools import lru_cache
 from typing import Optional
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -18,7 +19,8 @@ S2O_OK, S2O_EINVAL, S2O_EUNSUPPORTED, S2O_ESCRATCH, S2O_EHIP = 0, -1, -2, -3, -4
 STATIC_SCRATCH_BYTES = 32 << 20
 
 EXPORTS = ("s2o_version", "s2o_strerror", "s2o_last_hip_error", "s2o_plan_sizes", "s2o_plan", "s2o_plan_static",
-           "s2o_attention_sizes", "s2o_attention", "s2o_attention_local", "s2o_attention_prefix")
+           "s2o_attention_sizes", "s2o_attention", "s2o_attention_local", "s2o_attention_prefix",
+           "s2o_decode_sizes", "s2o_decode", "s2o_key_weights_sizes", "s2o_key_weights", "s2o_evict_sizes", "s2o_evict")
 
 
 class S2OParams(C.Structure):
@@ -35,6 +37,31 @@ class S2OPlanOut(C.Structure):
     _fields_ = [("q_perm", C.c_void_p), ("kv_perm", C.c_void_p), ("s_q", C.c_void_p),
                 ("s_k", C.c_void_p), ("q_mean", C.c_void_p), ("k_guide", C.c_void_p),
                 ("status", C.c_void_p)]
+
+
+S2O_BF16, S2O_F16 = 0, 1
+
+
+class S2ODecodeParams(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("struct_size", "batch", "branches", "q_heads", "kv_heads", "head_dim", "q_len", "cache_len",
+                                         "own_len", "dtype")] + [
+                ("softmax_scale", C.c_float), ("reserved", C.c_int32), ("q_stride", C.c_int64 * 4),
+                ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3), ("own_k_stride", C.c_int64 * 4),
+                ("own_v_stride", C.c_int64 * 4), ("o_stride", C.c_int64 * 4)]
+
+
+class S2OWeightsParams(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("struct_size", "batch", "branches", "q_heads", "kv_heads", "head_dim", "q_len", "cache_len",
+                                         "dtype", "causal")] + [
+                ("softmax_scale", C.c_float), ("reserved", C.c_int32), ("q_stride", C.c_int64 * 4),
+                ("k_stride", C.c_int64 * 3)]
+
+
+class S2OEvictParams(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("struct_size", "batch", "kv_heads", "head_dim", "cache_len", "keep", "sink", "recent", "dtype",
+                                         "reserved")] + [
+                ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3), ("out_k_stride", C.c_int64 * 3),
+                ("out_v_stride", C.c_int64 * 3)]
 
 
 class S2OError(RuntimeError):
@@ -79,6 +106,15 @@ def load_library():
     lib.s2o_attention_local.restype = C.c_int
     lib.s2o_attention_local.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(S2OParams),
                                         C.c_void_p, C.c_size_t, C.c_void_p]
+    vp, st = C.c_void_p, C.c_size_t
+    lib.s2o_decode_sizes.argtypes = [C.POINTER(S2ODecodeParams), szp, szp]
+    lib.s2o_decode.argtypes = [vp] * 7 + [C.POINTER(S2ODecodeParams), vp, vp, vp, st, vp]
+    lib.s2o_key_weights_sizes.argtypes = [C.POINTER(S2OWeightsParams), C.c_int, szp, szp]
+    lib.s2o_key_weights.argtypes = [vp] * 4 + [C.POINTER(S2OWeightsParams), vp, vp, vp, st, vp]
+    lib.s2o_evict_sizes.argtypes = [C.POINTER(S2OEvictParams), szp]
+    lib.s2o_evict.argtypes = [vp] * 4 + [C.POINTER(S2OEvictParams), vp, vp, vp, vp, vp, vp, st, vp]
+    for name in ("s2o_decode_sizes", "s2o_decode", "s2o_key_weights_sizes", "s2o_key_weights", "s2o_evict_sizes", "s2o_evict"):
+        getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
 
@@ -308,3 +344,275 @@ def s2o_attention_prefix(Q, K, V, params: S2OParams, q_perm, kv_perm, tau: float
                                     computed.data_ptr(), skipped.data_ptr(), _ptr(scratch),
                                     0 if scratch is None else scratch.numel(), _stream_handle(stream)))
     return O, computed, skipped
+
+
+# ---- the cache behind a prefill: s2o_decode, s2o_key_weights, s2o_evict
+
+def _dtype_code(dtype) -> int:
+    """"bf16" / "f16", the torch dtypes, or S2O_BF16 / S2O_F16."""
+    code = {"bf16": S2O_BF16, "f16": S2O_F16, "torch.bfloat16": S2O_BF16, "torch.float16": S2O_F16, "0": S2O_BF16, "1": S2O_F16}.get(str(dtype))
+    if code is None:
+        raise ValueError(f"dtype: expected bf16 or f16, got {dtype}")
+    return code
+
+
+def _filled_struct(p, strides, **fields):
+    p.struct_size = C.sizeof(p)
+    for name, val in fields.items():
+        setattr(p, name, val)
+    for name, val in strides.items():
+        kind = type(getattr(p, name))
+        if len(val) != kind._length_:
+            raise ValueError(f"{name}: expected {kind._length_} strides, got {len(val)}")
+        setattr(p, name, kind(*val))
+    return p
+
+
+def make_decode_params(Z, B, H, Hkv, D, T, L, own_len=0, dtype="bf16", softmax_scale=0.0, q_stride=(0,) * 4, k_stride=(0,) * 3,
+                       v_stride=(0,) * 3, own_k_stride=(0,) * 4, own_v_stride=(0,) * 4, o_stride=(0,) * 4) -> S2ODecodeParams:
+    """Z caches of at most L rows, B sequences on each with T query tokens and at most own_len rows of their own."""
+    return _filled_struct(S2ODecodeParams(), dict(q_stride=q_stride, k_stride=k_stride, v_stride=v_stride, own_k_stride=own_k_stride,
+                                                  own_v_stride=own_v_stride, o_stride=o_stride),
+                          batch=Z, branches=B, q_heads=H, kv_heads=Hkv, head_dim=D, q_len=T, cache_len=L, own_len=own_len,
+                          dtype=_dtype_code(dtype), softmax_scale=softmax_scale)
+
+
+def make_weights_params(Z, B, H, Hkv, D, T, L, dtype="bf16", causal=0, softmax_scale=0.0, q_stride=(0,) * 4,
+                        k_stride=(0,) * 3) -> S2OWeightsParams:
+    """Z caches of at most L rows, T query tokens of B sequences on each."""
+    return _filled_struct(S2OWeightsParams(), dict(q_stride=q_stride, k_stride=k_stride),
+                          batch=Z, branches=B, q_heads=H, kv_heads=Hkv, head_dim=D, q_len=T, cache_len=L, dtype=_dtype_code(dtype), causal=causal,
+                          softmax_scale=softmax_scale)
+
+
+def make_evict_params(Z, Hkv, D, L, keep, sink=0, recent=0, dtype="bf16", k_stride=(0,) * 3, v_stride=(0,) * 3, out_k_stride=(0,) * 3,
+                      out_v_stride=(0,) * 3) -> S2OEvictParams:
+    """Z caches of at most L rows that are cut down to at most `keep`."""
+    return _filled_struct(S2OEvictParams(), dict(k_stride=k_stride, v_stride=v_stride, out_k_stride=out_k_stride, out_v_stride=out_v_stride),
+                          batch=Z, kv_heads=Hkv, head_dim=D, cache_len=L, keep=keep, sink=sink, recent=recent, dtype=_dtype_code(dtype))
+
+
+def s2o_decode_sizes(params: S2ODecodeParams) -> dict:
+    a, b = C.c_size_t(0), C.c_size_t(0)
+    _check(load_library().s2o_decode_sizes(C.byref(params), C.byref(a), C.byref(b)))
+    return {"lse": int(a.value), "scratch": int(b.value)}
+
+
+def s2o_key_weights_sizes(params: S2OWeightsParams, with_lse: bool = False) -> dict:
+    """with_lse: of a call that is given the queries' lse (a call without it needs more)."""
+    a, b = C.c_size_t(0), C.c_size_t(0)
+    _check(load_library().s2o_key_weights_sizes(C.byref(params), int(with_lse), C.byref(a), C.byref(b)))
+    return {"weights": int(a.value), "scratch": int(b.value)}
+
+
+def s2o_evict_sizes(params: S2OEvictParams) -> dict:
+    b = C.c_size_t(0)
+    _check(load_library().s2o_evict_sizes(C.byref(params), C.byref(b)))
+    return {"scratch": int(b.value)}
+
+
+@lru_cache(maxsize=64)
+def _decode_layout(raw: bytes):
+    """What a call with these parameters (by value) takes: {name: (shape, strides or None for packed)}, scratch bytes."""
+    p = S2ODecodeParams.from_buffer_copy(raw)
+    scratch = s2o_decode_sizes(p)["scratch"]
+    q = (p.batch, p.branches, p.q_heads, p.q_len, p.head_dim)
+    k, own = (p.batch, p.kv_heads, p.cache_len, p.head_dim), (p.batch, p.branches, p.kv_heads, p.own_len, p.head_dim)
+    shapes = dict(Q=q, O=q, K=k, V=k, own_K=own, own_V=own)
+    return _with_strides(p, shapes, Q="q", O="o", K="k", V="v", own_K="own_k", own_V="own_v"), _torch_dtype(p.dtype), scratch
+
+
+@lru_cache(maxsize=64)
+def _weights_layout(raw: bytes, with_lse: bool):
+    p = S2OWeightsParams.from_buffer_copy(raw)
+    scratch = s2o_key_weights_sizes(p, with_lse)["scratch"]
+    shapes = dict(Q=(p.batch, p.branches, p.q_heads, p.q_len, p.head_dim), K=(p.batch, p.kv_heads, p.cache_len, p.head_dim))
+    return _with_strides(p, shapes, Q="q", K="k"), _torch_dtype(p.dtype), scratch
+
+
+@lru_cache(maxsize=64)
+def _evict_layout(raw: bytes):
+    p = S2OEvictParams.from_buffer_copy(raw)
+    scratch = s2o_evict_sizes(p)["scratch"]
+    k, out = (p.batch, p.kv_heads, p.cache_len, p.head_dim), (p.batch, p.kv_heads, p.keep, p.head_dim)
+    return _with_strides(p, dict(K=k, V=k, out_K=out, out_V=out), K="k", V="v", out_K="out_k", out_V="out_v"), _torch_dtype(p.dtype), scratch
+
+
+def _torch_dtype(code):
+    import torch
+    return torch.float16 if code == S2O_F16 else torch.bfloat16
+
+
+def _with_strides(p, shapes, **fields):
+    out = {}
+    for name, field in fields.items():
+        st = tuple(getattr(p, field + "_stride"))
+        out[name] = (shapes[name], st if any(st) else None)
+    return out
+
+
+def _check_layout(name, t, dtype, dev, shape, strides=None):
+    """The library sees only pointers: a tensor is what the parameters describe, or refused."""
+    if t.dtype is not dtype or not t.is_cuda or t.device != dev:
+        raise ValueError(f"{name}: expected a {dtype} tensor on {dev}, got {t.dtype} on {t.device}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected the shape {tuple(shape)}, got {tuple(t.shape)}")
+    if strides is None:
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: expected a packed tensor but this one is not contiguous (pass its strides in params or call "
+                             ".contiguous())")
+        return
+    have = t.stride()
+    if have[-1] != 1 or any(n > 1 and a != b for n, a, b in zip(shape, have, strides)):
+        raise ValueError(f"{name}: params describe the strides {strides}, but this tensor has {have}")
+
+
+def _on_device(dev, stream):
+    """(handle of the stream that the call goes to, context that makes `dev` the current device or None)."""
+    import torch
+    if stream is not None and getattr(stream, "device", dev) != dev:
+        raise ValueError(f"stream: on {stream.device}, the tensors on {dev}")
+    if dev.index == torch.cuda.current_device():
+        return _stream_handle(stream), None
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    return stream.cuda_stream or None, torch.cuda.device(dev)
+
+
+def _call(fn, ctx, *args):
+    if ctx is None:
+        return _check(fn(*args))
+    with ctx:
+        _check(fn(*args))
+
+
+def _scratch_for(scratch, size, dev, fresh):
+    import torch
+    if scratch is None and size:
+        scratch = torch.empty(size, dtype=torch.uint8, device=dev)
+        fresh.append(scratch)
+    if scratch is not None and (scratch.device != dev or not scratch.is_contiguous()):
+        raise ValueError(f"scratch: expected a contiguous tensor on {dev}")
+    return scratch, 0 if scratch is None else scratch.numel() * scratch.element_size()
+
+
+def s2o_decode(Q, K, V, params: S2ODecodeParams, own_K=None, own_V=None, lens=None, own_lens=None, O=None, lse=None, scratch=None,
+               stream=None, want_lse: bool = True):
+    """Attention of B sequences that share a cache, each with rows of its own behind it.  Q [Z,B,H,T,D]; K, V [Z,Hkv,L,D] or None
+    (params.cache_len 0); own_K, own_V [Z,B,Hkv,Lo,D] or None (params.own_len 0); lens [Z], own_lens [Z,B] int32: filled rows,
+    None for all.  Query t of T sees the shared rows and the own ones up to own_lens - T + t.
+    Returns (O like Q, lse [Z,B,H,T] fp32 or None); asynchronous on the current (or given) torch stream."""
+    import torch
+    lib = load_library()
+    layout, dtype, size = _decode_layout(bytes(params))
+    dev = Q.device
+    for name, t in (("Q", Q), ("K", K), ("V", V), ("own_K", own_K), ("own_V", own_V), ("O", O)):
+        if t is not None:
+            _check_layout(name, t, dtype, dev, *layout[name])
+    rows = layout["Q"][0][:4]
+    for name, t, kind, shape in (("lens", lens, torch.int32, rows[:1]), ("own_lens", own_lens, torch.int32, rows[:2]), ("lse", lse, torch.float32, rows)):
+        if t is not None:
+            _check_layout(name, t, kind, dev, shape)
+    fresh = []
+    if O is None:
+        shape, strides = layout["O"]
+        if strides is None:
+            O = torch.empty(shape, dtype=dtype, device=dev)
+        else:
+            O = torch.empty_strided(shape, strides + (1,), dtype=dtype, device=dev)
+        fresh.append(O)
+    if lse is None and want_lse:
+        lse = torch.empty(rows, dtype=torch.float32, device=dev)
+        fresh.append(lse)
+    scratch, size = _scratch_for(scratch, size, dev, fresh)
+    _keep_alive_on(stream, *fresh)
+    handle, ctx = _on_device(dev, stream)
+    _call(lib.s2o_decode, ctx, Q.data_ptr(), _ptr(K), _ptr(V), _ptr(own_K), _ptr(own_V), _ptr(lens), _ptr(own_lens), C.byref(params),
+          O.data_ptr(), _ptr(lse), _ptr(scratch), size, handle)
+    return O, lse
+
+
+def s2o_key_weights(Q, K, params: S2OWeightsParams, lse=None, lens=None, prev=None, out=None, scratch=None, stream=None):
+    """Softmax weights of a cache's keys added up over query rows: prev + sum exp(scale <q, k> - lse).  Q [Z,B,H,T,D]; K [Z,Hkv,L,D];
+    lse [Z,B,H,T] fp32 (as s2o_decode returns it) or None (of the keys a query sees here); lens [Z] int32 or None; prev
+    [Z,Hkv,L] fp32 or None; out like it, may be prev itself (entries behind lens are left as they were; without `out` they start at 0).
+    Returns out."""
+    import torch
+    lib = load_library()
+    layout, dtype, size = _weights_layout(bytes(params), lse is not None)
+    dev = Q.device
+    _check_layout("Q", Q, dtype, dev, *layout["Q"])
+    _check_layout("K", K, dtype, dev, *layout["K"])
+    shape = layout["K"][0][:3]
+    for name, t, kind, s in (("lse", lse, torch.float32, layout["Q"][0][:4]), ("lens", lens, torch.int32, shape[:1]), ("prev", prev, torch.float32, shape),
+                             ("out", out, torch.float32, shape)):
+        if t is not None:
+            _check_layout(name, t, kind, dev, s)
+    fresh = []
+    handle, ctx = _on_device(dev, stream)
+    if out is None:
+        if lens is None:
+            out = torch.empty(shape, dtype=torch.float32, device=dev)
+        elif stream is None:
+            out = torch.zeros(shape, dtype=torch.float32, device=dev)
+        else:
+            with torch.cuda.stream(stream):      # cleared where the kernels will run
+                out = torch.zeros(shape, dtype=torch.float32, device=dev)
+        fresh.append(out)
+    scratch, size = _scratch_for(scratch, size, dev, fresh)
+    _keep_alive_on(stream, *fresh)
+    _call(lib.s2o_key_weights, ctx, Q.data_ptr(), K.data_ptr(), _ptr(lse), _ptr(lens), C.byref(params), _ptr(prev), out.data_ptr(),
+          _ptr(scratch), size, handle)
+    return out
+
+
+@dataclass
+class Evicted:
+    K: "object"
+    V: "object"
+    weights: "object"            # [Z,Hkv,keep] fp32: the kept rows' weights
+    kept: "object"               # [Z,Hkv,keep] int32: their indices in the cache, ascending
+    lens: "object"               # [Z] int32: rows that are left
+
+
+def s2o_evict(K, V, weights, params: S2OEvictParams, lens=None, out_K=None, out_V=None, out_weights=None, kept=None, out_lens=None,
+              scratch=None, stream=None) -> Evicted:
+    """Cuts caches down to the first params.sink, the last params.recent and the otherwise most heavily weighted rows, params.keep in
+    all, in the order they had.  K, V [Z,Hkv,L,D] (both None: the selection alone); weights [Z,Hkv,L] fp32; lens [Z] int32 or None.
+    Outputs that are given are written into (out_K, out_V [Z,Hkv,keep,D]; rows behind the new lens are left as they were);
+    the others are allocated here, undefined behind the new lens."""
+    import torch
+    lib = load_library()
+    layout, dtype, size = _evict_layout(bytes(params))
+    dev = weights.device
+    if (K is None) != (V is None):
+        raise ValueError("K, V: both or neither")
+    if K is None and (out_K is not None or out_V is not None):
+        raise ValueError("out_K, out_V: nothing to move into them")
+    for name, t in (("K", K), ("V", V), ("out_K", out_K), ("out_V", out_V)):
+        if t is not None:
+            _check_layout(name, t, dtype, dev, *layout[name])
+    rows, left = layout["K"][0][:3], layout["out_K"][0][:3]
+    for name, t, kind, s in (("weights", weights, torch.float32, rows), ("lens", lens, torch.int32, rows[:1]), ("out_weights", out_weights, torch.float32, left),
+                             ("kept", kept, torch.int32, left), ("out_lens", out_lens, torch.int32, rows[:1])):
+        if t is not None:
+            _check_layout(name, t, kind, dev, s)
+    fresh = []
+
+    def new(t, shape, kind, strides=None):
+        if t is None:
+            t = torch.empty(shape, dtype=kind, device=dev) if strides is None else torch.empty_strided(shape, strides + (1,), dtype=kind, device=dev)
+            fresh.append(t)
+        return t
+
+    if K is not None:
+        (shape, ks), (_, vs) = layout["out_K"], layout["out_V"]
+        out_K, out_V = new(out_K, shape, dtype, ks), new(out_V, shape, dtype, vs)
+    out_weights, kept = new(out_weights, left, torch.float32), new(kept, left, torch.int32)
+    out_lens = new(out_lens, rows[:1], torch.int32)
+    scratch, size = _scratch_for(scratch, size, dev, fresh)
+    _keep_alive_on(stream, *fresh)
+    handle, ctx = _on_device(dev, stream)
+    _call(lib.s2o_evict, ctx, _ptr(K), _ptr(V), weights.data_ptr(), _ptr(lens), C.byref(params), _ptr(out_K), _ptr(out_V), out_weights.data_ptr(),
+          kept.data_ptr(), out_lens.data_ptr(), _ptr(scratch), size, handle)
+    return Evicted(out_K, out_V, out_weights, kept, out_lens)

@@ -8,7 +8,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libs2o.so")
-SOURCES = ["api.hip", "plan.hip", "attention.hip", "local.hip", "prefix.hip"]
+SOURCES = ["api.hip", "plan.hip", "attention.hip", "local.hip", "prefix.hip",
+           "cache_api.hip", "decode.hip", "weights.hip", "evict.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

@@ -9,13 +9,17 @@
 #include "s2o_internal.h"
 
 namespace {
-
 thread_local int g_last_hip_error = 0;
+}
 
-int hip_fail(hipError_t e) {
+int s2o::hip_fail(hipError_t e) {
   g_last_hip_error = (int)e;
   return S2O_EHIP;
 }
+
+namespace {
+
+using s2o::hip_fail;
 
 struct Shape {
   int Z, H, Hkv, L, D, S, N, nc;
@@ -117,7 +121,7 @@ const char* s2o_strerror(int code) {
   switch (code) {
     case S2O_OK: return "ok";
     case S2O_EINVAL: return "invalid argument";
-    case S2O_EUNSUPPORTED: return "unsupported configuration (need D=128, B_M in {64,128}, B_N=64, S%B_M==0; s2o_plan: S<=8192; no own-segment pass when non_causal)";
+    case S2O_EUNSUPPORTED: return "unsupported configuration (prefill: need D=128, B_M in {64,128}, B_N=64, S%B_M==0; s2o_plan: S<=8192; no own-segment pass when non_causal; cache: need D in {64,128}, K and V row strides < 16 MiB)";
     case S2O_ESCRATCH: return "scratch buffer missing, misaligned or too small (s2o_plan_static: the configuration needs more than the built-in S2O_STATIC_SCRATCH_BYTES)";
     case S2O_EHIP: return "HIP runtime error (see s2o_last_hip_error)";
     default: return "unknown error code";

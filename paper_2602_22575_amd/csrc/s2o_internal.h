@@ -93,4 +93,56 @@ hipError_t launch_local(const AttnArgs& a, hipStream_t stream);
 // Alg. 3 alone (prefix.hip): prefix walk in permuted query order from the state buffers
 hipError_t launch_prefix(const AttnArgs& a, hipStream_t stream);
 
+// Notes a failed HIP call for s2o_last_hip_error; S2O_EHIP.
+int hip_fail(hipError_t e);
+
+// s2o_decode (decode.hip).  qs, oks, ovs, os: strides for (z, b, head, row); ks, vs: (z, head, row).
+struct DecodeArgs {
+  const void *Q, *K, *V, *oK, *oV;
+  const int32_t *lens, *own_lens;
+  void* O;
+  float* lse;
+  int Z, B, H, Hkv, G, D, T, L, Lo, f16;
+  float c2;              // softmax_scale * log2(e)
+  int64_t qs[4], ks[3], vs[3], oks[4], ovs[4], os[4];
+  // set by the launch: states of the parts [part][row][D], {reference, sum} [part][row]; row blocks and parts of either kind
+  float* part_acc;
+  float2* part_ml;
+  int blocks_s, splits_s, blocks_o, splits_o, direct;
+};
+size_t decode_scratch_bytes(const DecodeArgs& a);
+hipError_t launch_decode(DecodeArgs a, void* scratch, hipStream_t stream);
+
+// s2o_key_weights (weights.hip)
+struct WeightsArgs {
+  const void *Q, *K;
+  const float *lse, *prev;
+  const int32_t* lens;
+  float* out;
+  int Z, B, H, Hkv, G, D, T, L, f16, causal;
+  float c2;              // softmax_scale * log2(e), and c2 / softmax_scale in two parts: what turns an lse into the scores' unit
+  float l2e_hi, l2e_lo;
+  int64_t qs[4], ks[3];
+  // set by the launch
+  float2* stats;         // [key part][cache, KV head][row]: {reference, sum}, joined: {reference, 1 / sum}
+  float* sums;           // [row part][cache, KV head][key]
+  int row_blocks, key_blocks, key_parts, row_parts;
+};
+size_t weights_scratch_bytes(WeightsArgs a, bool given);
+hipError_t launch_weights(WeightsArgs a, void* scratch, hipStream_t stream);
+
+// s2o_evict (evict.hip)
+struct EvictArgs {
+  const void *K, *V;
+  const float* weights;
+  const int32_t* lens;
+  void *K_out, *V_out;
+  float* weights_out;
+  int32_t *kept, *lens_out;
+  int Z, Hkv, D, L, keep, sink, recent;
+  int64_t ks[3], vs[3], kos[3], vos[3];
+};
+size_t evict_scratch_bytes(const EvictArgs& a);
+hipError_t launch_evict(const EvictArgs& a, void* scratch, hipStream_t stream);
+
 }  // namespace s2o
