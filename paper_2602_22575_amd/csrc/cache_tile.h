@@ -39,24 +39,29 @@ __device__ __forceinline__ int swz(int r) {
   if constexpr (D == 128) return ((r & 3) << 2) | ((((r >> 2) ^ (r >> 3)) & 1) << 1) | ((r >> 3) & 1);
   else return (((r >> 1) & 3) << 1) | ((r >> 3) & 1);
 }
-// byte address of chunk c of row r in a tile of rows of D elements
+// Byte address of chunk c of row r in a tile of rows of D elements.  swz(r + r') = swz(r) ^ swz(r') where r and r' share no bits, so
+// that addresses of one lane follow from a first one by an XOR with a constant.
 template <int D>
 __device__ __forceinline__ int at(int r, int c) { return r * (2 * D) + ((c ^ swz<D>(r)) << 4); }
+
+// Rows row0 .. row0 + most - 1 of a cache of `len` rows as a buffer: loads of rows behind the cache's end give zeros and touch no
+// memory.  Uniform arguments, row0 < len; `stride` in bytes, less than 2^24.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const void* cache, int64_t stride, int row0, int len, int most, int row_bytes) {
+  const char* p = static_cast<const char*>(cache) + row0 * stride;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, (uint32_t)(min(len - row0, most) - 1) * (uint32_t)stride + row_bytes, 0x00027000);
+}
+__device__ __forceinline__ u32x4 buffer_load(__amdgpu_buffer_rsrc_t b, uint32_t offset) {
+  return __builtin_amdgcn_raw_buffer_load_b128(b, offset, 0, 0);
+}
+__device__ __forceinline__ void buffer_load_to_lds(__amdgpu_buffer_rsrc_t b, uint32_t offset, unsigned char* lds) {
+  typedef __attribute__((address_space(3))) void lvoid;
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (lvoid*)lds, 16, offset, 0, 0, 0);
+}
 
 template <class E>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   typename Vec<E>::x2 t = {(E)lo, (E)hi};
   return __builtin_bit_cast(uint32_t, t);
-}
-
-// Any of the lane's 8 elements is infinite or NaN.
-template <class E>
-__device__ __forceinline__ bool not_finite(const u32x4& x) {
-  const uint32_t e = sizeof(E) == 2 && __is_same(E, __bf16) ? 0x7f80u : 0x7c00u;
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) bad |= (x[i] & e) == e || ((x[i] >> 16) & e) == e;
-  return bad;
 }
 
 // Over the four lanes l % 16 + 16 * {0..3} that share a column of an accumulator block.

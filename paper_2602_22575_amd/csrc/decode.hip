@@ -11,9 +11,14 @@
 // un-normalised softmax state (accumulator, maximum, sum) per query row and part; a second launch joins the parts.  Where
 // all keys are few, a workgroup walks a sequence's shared and own rows in turn and writes the result itself.
 //
-// A wavefront walks tiles of 32 keys of its own, without barriers: K operands come straight from global memory (16 rows x 64
-// bytes an instruction), V passes through a wavefront's private 32 x D of LDS for the transposing read.  The next
-// tile's loads are issued as soon as the score products have consumed the current ones.  Bound: HBM bandwidth.
+// A row block of up to 16 rows is walked by wavefronts on their own (Walk::narrow): each takes tiles of 32 keys in turn, without
+// barriers; K operands come straight from global memory (16 rows x 64 bytes an instruction), V passes through a wavefront's
+// private 32 x D of LDS for the transposing read.  The next tile's loads are issued as soon as the score products have consumed the
+// current ones.  Bound: HBM bandwidth.
+// Blocks of 128 rows share tiles of 64 keys between four wavefronts of 32 rows each (Walk::wide): global memory goes
+// straight to LDS, one tile ahead.  Bound: HBM bandwidth up to about 256 rows a KV head, the matrix cores beyond.
+#include <type_traits>
+
 #include "cache_tile.h"
 #include "s2o_internal.h"
 
@@ -23,7 +28,9 @@ namespace {
 
 using namespace cache;
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves, kKeys = 32;
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kKeys = 32, kWideKeys = 64;       // tiles of the two walks
+constexpr int kNarrowRows = 16, kWideRows = 32 * kWaves;   // query rows of a workgroup
 constexpr float kLazy = 8.0f;    // the softmax reference follows the maximum in steps of 2^8 at least (attn_tile.h)
 
 // Query rows of a workgroup: those of one sequence (b >= 0) or of all that read the cache, with t the slowest index.
@@ -37,6 +44,7 @@ struct Rows {
   }
 };
 
+// The softmax state of 16 * CB query rows in a wavefront (column cb of lane l: row 16 * cb + l % 16).
 template <class E, int D, int CB>
 struct Walk {
   typedef typename Vec<E>::x8 x8;
@@ -54,50 +62,139 @@ struct Walk {
     }
   }
 
-  // Tiles first, first + step, .. < end of a cache of `len` rows; the lane's column cb sees the first lim[cb] of them.
-  // vt: the wavefront's 32 x D elements of LDS.
-  __device__ __forceinline__ void tiles(const E* K, const E* V, int64_t kstride, int64_t vstride, int len, const int (&lim)[CB],
-                                        int first, int end, int step, float c2, unsigned char* vt, int lane) {
+  // Scores of KB blocks of 16 keys -> softmax numerators (in s, fp32) and their rounding for the second product (half a step of the cache's
+  // own type; the sums are of the unrounded ones).  The reference follows the maximum lazily; sums stay per lane until the end.
+  template <int KB, bool kHidden>
+  __device__ __forceinline__ void softmax(f32x4 (&s)[KB][CB], x8 (&pb)[KB / 2][CB], int key0, const int (&lim)[CB], float c2, int g) {
+    if constexpr (kHidden) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (key0 + 16 * kb + 4 * g + i >= lim[cb]) s[kb][cb][i] = -INFINITY;
+    }
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[kb][cb][i]);
+      top = column_max(top) * c2;
+      const bool grow = top > m[cb] + kLazy;
+      if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+        const float m_new = grow ? top : m[cb];
+        const float alpha = grow ? exp2_(m[cb] - m_new) : 1.0f;
+        m[cb] = m_new;
+        l[cb] *= alpha;
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[cb][db][i] *= alpha;
+      }
+      const float ref = m[cb] == -INFINITY ? 0.f : m[cb];
+      float sum = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p = exp2_(fmaf(s[kb][cb][i], c2, -ref));
+          s[kb][cb][i] = p;
+          sum += p;
+        }
+      l[cb] += sum;
+#pragma unroll
+      for (int st = 0; st < KB / 2; ++st) {
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = pack2<E>(s[2 * st + (j >> 1)][cb][2 * (j & 1)], s[2 * st + (j >> 1)][cb][2 * (j & 1) + 1]);
+        pb[st][cb] = __builtin_bit_cast(x8, w);
+      }
+    }
+  }
+
+  // The V^T operand of 16 dims and 32 keys whose rows start at `vt` in LDS: keys 4 * g + (0..3) and 16 + 4 * g + (0..3).
+  static __device__ __forceinline__ u32x4 value_operand(const unsigned char* vt, int db, int mm, int g) {
+    typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+    const unsigned char* p = vt + ((at<D>(4 * g + (mm >> 2), (mm & 3) >> 1) + 8 * (mm & 1)) ^ (db << 5));
+    const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
+    const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 16 * 2 * D));
+    const u32x2 w0 = __builtin_bit_cast(u32x2, v0), w1 = __builtin_bit_cast(u32x2, v1);
+    return u32x4{w0.x, w0.y, w1.x, w1.y};
+  }
+  // O^T += V^T P^T for 32 * ST keys
+  template <int ST>
+  __device__ __forceinline__ void values(const unsigned char* vt, const x8 (&pb)[ST][CB], int mm, int g) {
+#pragma unroll
+    for (int st = 0; st < ST; ++st)
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) {
+        const x8 vf = __builtin_bit_cast(x8, value_operand(vt + st * 64 * D, db, mm, g));
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) o[cb][db] = mfma(vf, pb[st][cb], o[cb][db]);
+      }
+  }
+  // The same where some column does not see all of the keys.  A row that a column does not see has p = 0 there, but may hold an infinity or
+  // NaN: per limit that occurs (one, but for the last tokens of several) a product with the rows behind it as zeros, added to
+  // the columns of that limit.
+  template <int ST>
+  __device__ __forceinline__ void values_hidden(const unsigned char* vt, const x8 (&pb)[ST][CB], int key0, const int (&lim)[CB], int mm, int g) {
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      uint64_t todo = ~0ull;
+      while (todo) {
+        const int u = __builtin_amdgcn_readlane(lim[cb], __builtin_ctzll(todo));
+        const bool mine = lim[cb] == u;
+        todo &= ~__builtin_amdgcn_ballot_w64(mine);
+#pragma unroll
+        for (int st = 0; st < ST; ++st)
+#pragma unroll
+          for (int db = 0; db < D / 16; ++db) {
+            u32x4 v = value_operand(vt + st * 64 * D, db, mm, g);
+            const int left = u - key0 - 32 * st - 4 * g;             // of the operand's keys 0..3, 16..19
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int key = 16 * (j >> 1) + 2 * (j & 1);
+              v[j] = key + 1 < left ? v[j] : key < left ? v[j] & 0xffffu : 0u;
+            }
+            const f32x4 sum = mfma(__builtin_bit_cast(x8, v), pb[st][cb], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[cb][db][i] += mine ? sum[i] : 0.f;
+          }
+      }
+    }
+  }
+
+  // Tiles first, first + step, .. < end of a cache of `len` rows; the lane's column cb sees the first lim[cb] of them, every column the
+  // first lim_all.  vt: the wavefront's 32 x D elements of LDS.
+  // (The tiles that some column does not see all of, the last ones, have a loop of their own here and in `wide`: what they need
+  // beside the products would cost every tile registers.)
+  __device__ __forceinline__ void narrow(const E* K, const E* V, int64_t kstride, int64_t vstride, int len, const int (&lim)[CB], int lim_all,
+                                         int first, int end, int step, float c2, unsigned char* vt, int lane) {
     constexpr int kRowLanes = D / 8, kLoads = D / 16;      // 16-byte pieces a row; V loads a lane
     constexpr int kRowsPerLoad = 64 / kRowLanes;
-    const int mm = lane & 15, g = lane >> 4;
+    const int mm = lane & 15, g = lane >> 4, lr = lane / kRowLanes;
     u32x4 kr[2][D / 32], vr[kLoads];
-    const uint32_t krow = (uint32_t)(kstride * 2), vrow = (uint32_t)(vstride * 2);
+    const uint32_t koff = (uint32_t)mm * (uint32_t)(kstride * 2) + 16 * g, voff = (uint32_t)lr * (uint32_t)(vstride * 2) + 16 * (lane % kRowLanes);
+    const int vst = at<D>(lr, lane % kRowLanes);
     auto load = [&](int t) {
-      const char* kt = reinterpret_cast<const char*>(K + (int64_t)t * kKeys * kstride);
-      const char* vtile = reinterpret_cast<const char*>(V + (int64_t)t * kKeys * vstride);
-      const int last = len - 1 - t * kKeys;                // rows behind the cache's end are not read: the last one instead
+      const auto kt = rows_buffer(K, kstride * 2, t * kKeys, len, kKeys, 2 * D), vtile = rows_buffer(V, vstride * 2, t * kKeys, len, kKeys, 2 * D);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const uint32_t off = (uint32_t)min(16 * kb + mm, last) * krow + 16 * g;
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int kk = 0; kk < D / 32; ++kk) kr[kb][kk] = *reinterpret_cast<const u32x4*>(kt + off + 64 * kk);
-      }
+        for (int kk = 0; kk < D / 32; ++kk) kr[kb][kk] = buffer_load(kt, koff + 16 * kb * (uint32_t)(kstride * 2) + 64 * kk);
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const uint32_t off = (uint32_t)min(kRowsPerLoad * i + lane / kRowLanes, last) * vrow + 16 * (lane % kRowLanes);
-        vr[i] = *reinterpret_cast<const u32x4*>(vtile + off);
-      }
+      for (int i = 0; i < kLoads; ++i) vr[i] = buffer_load(vtile, voff + kRowsPerLoad * i * (uint32_t)(vstride * 2));
     };
-    if (first < end) load(first);
-    for (int t = first; t < end; t += step) {
+    auto tile = [&](int t, auto hidden_) {
+      constexpr bool kHidden = decltype(hidden_)::value;
       const int key0 = t * kKeys;
-      bool hidden = false;                                 // some row of this tile is not seen by some column
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb) hidden |= lim[cb] < key0 + kKeys;
-      hidden = __builtin_amdgcn_ballot_w64(hidden) != 0;
-      bool odd_values = false;
       wave_fence();                                        // the last tile's reads are through
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int r = kRowsPerLoad * i + lane / kRowLanes;
-        u32x4 v = vr[i];
-        if (hidden) {
-          if (key0 + r >= len) v = u32x4{0, 0, 0, 0};
-          odd_values |= not_finite<E>(v);
-        }
-        *reinterpret_cast<u32x4*>(vt + at<D>(r, lane % kRowLanes)) = v;
-      }
+      for (int i = 0; i < kLoads; ++i)
+        *reinterpret_cast<u32x4*>(vt + kRowsPerLoad * i * 2 * D + (vst ^ (swz<D>(kRowsPerLoad * i) << 4))) = vr[i];
       wave_fence();
       f32x4 s[2][CB];
 #pragma unroll
@@ -108,84 +205,79 @@ struct Walk {
 #pragma unroll
           for (int kk = 0; kk < D / 32; ++kk) s[kb][cb] = mfma(__builtin_bit_cast(x8, kr[kb][kk]), q[cb][kk], s[kb][cb]);
         }
+      __builtin_amdgcn_sched_barrier(0);                   // (the loads take over the products' operand registers)
       if (t + step < end) load(t + step);
-      if (hidden) {
+      x8 pb[1][CB];
+      softmax<2, kHidden>(s, pb, key0, lim, c2, g);
+      if constexpr (kHidden) values_hidden<1>(vt, pb, key0, lim, mm, g);
+      else values<1>(vt, pb, mm, g);
+    };
+    if (first < end) load(first);
+    int t = first;
+    for (; t < end && (t + 1) * kKeys <= lim_all; t += step) tile(t, std::false_type{});
+    for (; t < end; t += step) tile(t, std::true_type{});
+  }
+
+  // Tiles from .. to - 1 of 64 keys, by all four wavefronts together.  ka, kb_, va, vb: K and V tile of even and odd steps (separate
+  // arrays, so that the compiler sees that reads of one need not wait for the loads that fill another).
+  __device__ __forceinline__ void wide(const E* K, const E* V, int64_t kstride, int64_t vstride, int len, const int (&lim)[CB], int lim_all,
+                                       int from, int to, float c2, unsigned char* ka, unsigned char* kb_, unsigned char* va, unsigned char* vb, int wave, int lane) {
+    constexpr int kRowLanes = D / 8, kRowsPerLoad = 64 / kRowLanes, kLoads = 16 / kRowsPerLoad;   // a wavefront loads 16 rows of each
+    const int mm = lane & 15, g = lane >> 4, lr = lane / kRowLanes;
+    // LDS takes a load's lanes in order: each fetches the chunk that belongs at its slot
+    const uint32_t chunk = 16 * ((lane % kRowLanes) ^ swz<D>(lr));
+    const uint32_t krow = (uint32_t)(kstride * 2), vrow = (uint32_t)(vstride * 2), koff = (uint32_t)lr * krow, voff = (uint32_t)lr * vrow;
+    auto fetch = [&](int t, unsigned char* kt, unsigned char* vt) {
+      const auto kg = rows_buffer(K, kstride * 2, t * kWideKeys, len, kWideKeys, 2 * D), vg = rows_buffer(V, vstride * 2, t * kWideKeys, len, kWideKeys, 2 * D);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (key0 + 16 * kb + 4 * g + i >= lim[cb]) s[kb][cb][i] = -INFINITY;
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = 16 * wave + kRowsPerLoad * i;
+        const uint32_t c = chunk ^ (swz<D>(kRowsPerLoad * i) << 4);
+        buffer_load_to_lds(kg, koff + r * krow + c, kt + r * 2 * D);
+        buffer_load_to_lds(vg, voff + r * vrow + c, vt + r * 2 * D);
       }
-      // softmax numerators against a lazily moving reference; the sums stay per lane until the end
-      x8 pb[CB];
+    };
+    // what this wavefront fetched has landed and what it read is in its registers; then everybody's
+    auto meet = [] {
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0x0070);                  // vmcnt(0) lgkmcnt(0)
+      asm volatile("s_barrier" ::: "memory");
+    };
+    auto step = [&](int t, unsigned char* kt, unsigned char* vt, unsigned char* knext, unsigned char* vnext, auto hidden_) {
+      constexpr bool kHidden = decltype(hidden_)::value;
+      if (t + 1 < to) fetch(t + 1, knext, vnext);
+      const int key0 = t * kWideKeys;
+      f32x4 s[4][CB];
 #pragma unroll
-      for (int cb = 0; cb < CB; ++cb) {
-        float top = fmaxf(fmaxf(fmaxf(s[0][cb][0], s[0][cb][1]), fmaxf(s[0][cb][2], s[0][cb][3])),
-                          fmaxf(fmaxf(s[1][cb][0], s[1][cb][1]), fmaxf(s[1][cb][2], s[1][cb][3])));
-        top = column_max(top) * c2;
-        const bool grow = top > m[cb] + kLazy;
-        if (__builtin_amdgcn_ballot_w64(grow) != 0) {
-          const float m_new = grow ? top : m[cb];
-          const float alpha = grow ? exp2_(m[cb] - m_new) : 1.0f;
-          m[cb] = m_new;
-          l[cb] *= alpha;
+      for (int kb = 0; kb < 4; ++kb) {
+        x8 k[D / 32];
 #pragma unroll
-          for (int db = 0; db < D / 16; ++db)
+        for (int kk = 0; kk < D / 32; ++kk) k[kk] = *reinterpret_cast<const x8*>(kt + 16 * kb * 2 * D + (at<D>(mm, g) ^ (kk << 6)));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[cb][db][i] *= alpha;
-        }
-        const float ref = m[cb] == -INFINITY ? 0.f : m[cb];
-        float sum = 0.f;
+        for (int cb = 0; cb < CB; ++cb) {
+          s[kb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p = exp2_(fmaf(s[kb][cb][i], c2, -ref));
-            s[kb][cb][i] = p;
-            sum += p;
-          }
-        l[cb] += sum;
-        // rounded for the second product (half a step of the cache's own type); the sum is of the unrounded ones
-        u32x4 w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = pack2<E>(s[j >> 1][cb][2 * (j & 1)], s[j >> 1][cb][2 * (j & 1) + 1]);
-        pb[cb] = __builtin_bit_cast(x8, w);
-      }
-      if (hidden && __builtin_amdgcn_ballot_w64(odd_values) != 0) {
-        // An infinity or NaN in a row that some column does not see must not reach it as 0 * inf: key by key, hidden
-        // ones left out.
-#pragma unroll 1
-        for (int r = 0; r < kKeys; ++r) {
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb) {
-              const f32x4 sv = r >= 16 ? s[1][cb] : s[0][cb];
-              const float mine = (r & 3) == 0 ? sv[0] : (r & 3) == 1 ? sv[1] : (r & 3) == 2 ? sv[2] : sv[3];
-              const float p = __shfl(mine, 16 * ((r & 15) >> 2) + mm);
-              if (key0 + r < lim[cb])
-#pragma unroll
-                for (int db = 0; db < D / 16; ++db) {
-                  const E* v = reinterpret_cast<const E*>(vt + at<D>(r, 2 * db + (g >> 1)) + 8 * (g & 1));
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) o[cb][db][i] = fmaf(p, (float)v[i], o[cb][db][i]);
-                }
-            }
-          }
-      } else {
-        const int rl = 4 * g + (mm >> 2);
-#pragma unroll
-        for (int db = 0; db < D / 16; ++db) {
-          typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-          const int c = 2 * db + ((mm & 3) >> 1), in = 8 * (mm & 1);
-          const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vt + at<D>(rl, c) + in));
-          const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vt + at<D>(16 + rl, c) + in));
-          const u32x2 w0 = __builtin_bit_cast(u32x2, v0), w1 = __builtin_bit_cast(u32x2, v1);
-          const x8 vf = __builtin_bit_cast(x8, u32x4{w0.x, w0.y, w1.x, w1.y});
-#pragma unroll
-          for (int cb = 0; cb < CB; ++cb) o[cb][db] = mfma(vf, pb[cb], o[cb][db]);
+          for (int kk = 0; kk < D / 32; ++kk) s[kb][cb] = mfma(k[kk], q[cb][kk], s[kb][cb]);
         }
       }
+      x8 pb[2][CB];
+      softmax<4, kHidden>(s, pb, key0, lim, c2, g);
+      if constexpr (kHidden) values_hidden<2>(vt, pb, key0, lim, mm, g);
+      else values<2>(vt, pb, mm, g);
+      meet();
+    };
+    if (from >= to) return;
+    fetch(from, ka, va);
+    meet();
+    const int full = min(to, max(from, lim_all / kWideKeys));
+    int t = from;
+    for (; t < full; t += 2) {
+      step(t, ka, va, kb_, vb, std::false_type{});
+      if (t + 1 < full) step(t + 1, kb_, vb, ka, va, std::false_type{});
+    }
+    for (t = full; t < to; ++t) {
+      const bool odd = (t - from) & 1;
+      step(t, odd ? kb_ : ka, odd ? vb : va, odd ? ka : kb_, odd ? va : vb, std::true_type{});
     }
   }
 };
@@ -197,128 +289,205 @@ __device__ __forceinline__ float natural_lse(float top, float sum) {
   return sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-template <class E, int D, int CB>
-__global__ __launch_bounds__(kThreads, 2) void decode_kernel(const DecodeArgs a) {
-  constexpr int kPad = D + 4;
-  constexpr int kTile = kKeys * D * 2;
-  constexpr int kJoin = kWaves * 16 * kPad * 4;
-  __shared__ __attribute__((aligned(256))) unsigned char smem[kWaves * kTile > kJoin ? kWaves * kTile : kJoin];
-  __shared__ float2 ml[kWaves][16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int mm = lane & 15, g = lane >> 4;
-
-  // block id -> shared units (cache, KV head, row block) x parts, then own units (.., sequence, ..) x parts
-  const int units_s = a.Z * a.Hkv * a.blocks_s;
-  int id = blockIdx.x, part;
+// kWideS, kWideO: shared / own row blocks are walked 128 rows at a time, else 16.  Both kinds of block in one launch: the long
+// shared ones first.
+template <class E, int D>
+struct Block {
+  const DecodeArgs& a;
   Rows rows;
-  int rb;
-  bool shared = !a.direct && id < units_s * a.splits_s;
-  if (shared) {
-    part = id / units_s;
-    id -= part * units_s;
-    rb = id % a.blocks_s;
-    id /= a.blocks_s;
-    rows.g = id % a.Hkv;
-    rows.z = id / a.Hkv;
-    rows.b = -1;
-    rows.count = a.B * a.T * a.G;
-  } else {
-    if (!a.direct) id -= units_s * a.splits_s;
-    const int units_o = a.Z * a.B * a.Hkv * a.blocks_o;
-    part = id / units_o;
-    id -= part * units_o;
-    rb = id % a.blocks_o;
-    id /= a.blocks_o;
-    rows.g = id % a.Hkv;
-    id /= a.Hkv;
-    rows.b = id % a.B;
-    rows.z = id / a.B;
-    rows.count = a.T * a.G;
-  }
-  const int z = rows.z, hk = rows.g;
+  int rb, part, slot;
+  bool shared;
 
-  Walk<E, D, CB> w;
-  w.start();
-  int t_of[CB];
-  const E* Q = static_cast<const E*>(a.Q);
+  // Part and result of the row that (the lane's group of) D / 16 threads hold.
+  __device__ __forceinline__ void write(int r, int d0, const float (&acc)[D / 16], float top, float sum, bool first) const {
+    int b, h, t;
+    rows.find(a, r, b, h, t);
+    const int z = rows.z;
+    const int64_t all_rows = (int64_t)a.Z * a.B * a.H * a.T, row = (((int64_t)z * a.B + b) * a.H + h) * a.T + t;
+    if (a.part_acc) {
+      float* p = a.part_acc + (slot * all_rows + row) * D + d0;
 #pragma unroll
-  for (int cb = 0; cb < CB; ++cb) {
-    int b, h;
-    rows.find(a, min(16 * (rb * CB + cb) + mm, rows.count - 1), b, h, t_of[cb]);
-    const E* q = Q + z * a.qs[0] + b * a.qs[1] + h * a.qs[2] + t_of[cb] * a.qs[3];
+      for (int d = 0; d < D / 16; d += 4) *reinterpret_cast<f32x4*>(p + d) = f32x4{acc[d], acc[d + 1], acc[d + 2], acc[d + 3]};
+      if (first) a.part_ml[slot * all_rows + row] = float2{top, sum};
+    } else {
+      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+      uint32_t* o = reinterpret_cast<uint32_t*>(static_cast<E*>(a.O) + z * a.os[0] + b * a.os[1] + h * a.os[2] + t * a.os[3] + d0);
 #pragma unroll
-    for (int kk = 0; kk < D / 32; ++kk) w.q[cb][kk] = *reinterpret_cast<const typename Vec<E>::x8*>(q + 32 * kk + 8 * g);
+      for (int d = 0; d < D / 16; d += 2) o[d / 2] = pack2<E>(acc[d] * inv, acc[d + 1] * inv);
+      if (a.lse && first) a.lse[row] = natural_lse(top, sum);
+    }
   }
-  unsigned char* vt = smem + wave * kTile;
-  // the shared rows, the sequence's own, or both
-#pragma unroll 1
-  for (int own = shared || a.direct ? 0 : 1; own < (shared ? 1 : 2); ++own) {
+
+  // Loads the query rows from r0 on into the columns of `w`; tokens of the rows.
+  template <int CB>
+  __device__ __forceinline__ void load(Walk<E, D, CB>& w, int r0, int (&t_of)[CB], int lane) const {
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      int b, h;
+      rows.find(a, min(r0 + 16 * cb + (lane & 15), rows.count - 1), b, h, t_of[cb]);
+      const E* q = static_cast<const E*>(a.Q) + rows.z * a.qs[0] + b * a.qs[1] + h * a.qs[2] + t_of[cb] * a.qs[3];
+#pragma unroll
+      for (int kk = 0; kk < D / 32; ++kk) w.q[cb][kk] = *reinterpret_cast<const typename Vec<E>::x8*>(q + 32 * kk + 8 * (lane >> 4));
+    }
+  }
+
+  // The cache that the block walks (own: its sequence's), and this part's tiles of `keys` rows.
+  struct Cache {
     const E *K, *V;
     int64_t kst, vst;
-    int len, splits = 1, lim[CB];
+    int len, from, to;
+  };
+  __device__ __forceinline__ Cache cache(bool own, int keys) const {
+    const int z = rows.z, hk = rows.g, b = rows.b;
+    Cache c;
+    int splits = 1;
     if (own) {
-      K = static_cast<const E*>(a.oK) + z * a.oks[0] + rows.b * a.oks[1] + hk * a.oks[2];
-      V = static_cast<const E*>(a.oV) + z * a.ovs[0] + rows.b * a.ovs[1] + hk * a.ovs[2];
-      kst = a.oks[3]; vst = a.ovs[3];
-      len = filled(a.own_lens, z * a.B + rows.b, a.Lo);
+      c.K = static_cast<const E*>(a.oK) + z * a.oks[0] + b * a.oks[1] + hk * a.oks[2];
+      c.V = static_cast<const E*>(a.oV) + z * a.ovs[0] + b * a.ovs[1] + hk * a.ovs[2];
+      c.kst = a.oks[3]; c.vst = a.ovs[3];
+      c.len = filled(a.own_lens, z * a.B + b, a.Lo);
       if (!a.direct) splits = a.splits_o;
     } else {
-      K = static_cast<const E*>(a.K) + z * a.ks[0] + hk * a.ks[1];
-      V = static_cast<const E*>(a.V) + z * a.vs[0] + hk * a.vs[1];
-      kst = a.ks[2]; vst = a.vs[2];
-      len = filled(a.lens, z, a.L);
+      c.K = static_cast<const E*>(a.K) + z * a.ks[0] + hk * a.ks[1];
+      c.V = static_cast<const E*>(a.V) + z * a.vs[0] + hk * a.vs[1];
+      c.kst = a.ks[2]; c.vst = a.vs[2];
+      c.len = filled(a.lens, z, a.L);
       if (!a.direct) splits = a.splits_s;
     }
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) lim[cb] = own ? min(max(len - a.T + t_of[cb] + 1, 0), len) : len;
-    const int tiles = (len + kKeys - 1) / kKeys;
-    const int from = (int)((int64_t)tiles * part / splits), to = (int)((int64_t)tiles * (part + 1) / splits);
-    w.tiles(K, V, kst, vst, len, lim, from + wave, to, kWaves, a.c2, vt, lane);
+    const int tiles = (c.len + keys - 1) / keys;
+    c.from = (int)((int64_t)tiles * part / splits);
+    c.to = (int)((int64_t)tiles * (part + 1) / splits);
+    return c;
   }
+  // rows that query token t sees; what the row block's first row does, all do
+  __device__ __forceinline__ int limit(const Cache& c, bool own, int t) const { return own ? min(max(c.len - a.T + t + 1, 0), c.len) : c.len; }
+};
 
-  // join the wavefronts, 16 rows at a time
-  const int64_t all_rows = (int64_t)a.Z * a.B * a.H * a.T;
-  const int slot = shared ? part : a.splits_s + part;
+// `area(v)`: 32 x D elements of LDS for wavefront v.
+template <class E, int D, class F>
+__device__ __forceinline__ void narrow_block(const Block<E, D>& k, F area, float2 (*ml)[16], int tid) {
+  const DecodeArgs& a = k.a;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), mm = lane & 15, g = lane >> 4;
+  Walk<E, D, 1> w;
+  w.start();
+  int t_of[1];
+  k.load(w, kNarrowRows * k.rb, t_of, lane);
+  // the shared rows, the sequence's own, or both
+#pragma unroll 1
+  for (int own = k.shared || a.direct ? 0 : 1; own < (k.shared ? 1 : 2); ++own) {
+    const auto c = k.cache(own, kKeys);
+    const int lim[1] = {k.limit(c, own, t_of[0])};
+    w.narrow(c.K, c.V, c.kst, c.vst, c.len, lim, k.limit(c, own, kNarrowRows * k.rb / a.G), c.from + wave, c.to, kWaves, a.c2, area(wave), lane);
+  }
+  // join the wavefronts: 16 rows x D in 32 bits fill a wavefront's area; the 16-byte pieces of row r sit at piece ^ r
+  __syncthreads();
+  const float l = column_sum(w.l[0]);
 #pragma unroll
-  for (int cb = 0; cb < CB; ++cb) {
-    __syncthreads();
-    float* ob = reinterpret_cast<float*>(smem);
-    const float l = column_sum(w.l[cb]);
+  for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4*>(area(wave) + mm * (4 * D) + (((4 * db + g) ^ mm) << 4)) = w.o[0][db];
+  if (g == 0) ml[wave][mm] = float2{w.m[0], l};
+  __syncthreads();
+  const int i = tid >> 4, r = kNarrowRows * k.rb + i, d0 = (tid & 15) * (D / 16);
+  if (r >= k.rows.count) return;
+  float top = -INFINITY, sum = 0.f, acc[D / 16];
 #pragma unroll
-    for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4*>(ob + (wave * 16 + mm) * kPad + 16 * db + 4 * g) = w.o[cb][db];
-    if (g == 0) ml[wave][mm] = float2{w.m[cb], l};
-    __syncthreads();
-    const int i = tid >> 4, r = 16 * (rb * CB + cb) + i, d0 = (tid & 15) * (D / 16);
-    if (r < rows.count) {
-      float top = -INFINITY, sum = 0.f;
+  for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ml[v][i].x);
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ml[v][i].x);
-      float acc[D / 16];
+  for (int d = 0; d < D / 16; ++d) acc[d] = 0.f;
 #pragma unroll
-      for (int d = 0; d < D / 16; ++d) acc[d] = 0.f;
+  for (int v = 0; v < kWaves; ++v) {
+    const float f = part_weight(ml[v][i].x, top);
+    sum = fmaf(f, ml[v][i].y, sum);
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) {
-        const float f = part_weight(ml[v][i].x, top);
-        sum = fmaf(f, ml[v][i].y, sum);
+    for (int d = 0; d < D / 16; d += 4) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(area(v) + i * (4 * D) + ((((d0 + d) / 4) ^ i) << 4));
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) acc[d] = fmaf(f, ob[(v * 16 + i) * kPad + d0 + d], acc[d]);
-      }
-      int b, h, t;
-      rows.find(a, r, b, h, t);
-      const int64_t row = (((int64_t)z * a.B + b) * a.H + h) * a.T + t;
-      if (a.part_acc) {
-        float* p = a.part_acc + (slot * all_rows + row) * D + d0;
-#pragma unroll
-        for (int d = 0; d < D / 16; d += 4) *reinterpret_cast<f32x4*>(p + d) = f32x4{acc[d], acc[d + 1], acc[d + 2], acc[d + 3]};
-        if ((tid & 15) == 0) a.part_ml[slot * all_rows + row] = float2{top, sum};
-      } else {
-        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        uint32_t* o = reinterpret_cast<uint32_t*>(static_cast<E*>(a.O) + z * a.os[0] + b * a.os[1] + h * a.os[2] + t * a.os[3] + d0);
-#pragma unroll
-        for (int d = 0; d < D / 16; d += 2) o[d / 2] = pack2<E>(acc[d] * inv, acc[d + 1] * inv);
-        if (a.lse && (tid & 15) == 0) a.lse[row] = natural_lse(top, sum);
-      }
+      for (int j = 0; j < 4; ++j) acc[d + j] = fmaf(f, x[j], acc[d + j]);
     }
+  }
+  k.write(r, d0, acc, top, sum, (tid & 15) == 0);
+}
+
+template <class E, int D>
+__device__ __forceinline__ void wide_block(const Block<E, D>& k, unsigned char* ka, unsigned char* kb, unsigned char* va, unsigned char* vb, int tid) {
+  const DecodeArgs& a = k.a;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), mm = lane & 15, g = lane >> 4;
+  const int r0 = kWideRows * k.rb + 32 * wave;
+  Walk<E, D, 2> w;
+  w.start();
+  int t_of[2];
+  k.load(w, r0, t_of, lane);
+#pragma unroll 1
+  for (int own = k.shared || a.direct ? 0 : 1; own < (k.shared ? 1 : 2); ++own) {
+    const auto c = k.cache(own, kWideKeys);
+    const int lim[2] = {k.limit(c, own, t_of[0]), k.limit(c, own, t_of[1])};
+    w.wide(c.K, c.V, c.kst, c.vst, c.len, lim, k.limit(c, own, kWideRows * k.rb / a.G), c.from, c.to, a.c2, ka, kb, va, vb, wave, lane);
+  }
+  // O^T to rows: lane l's piece of row l % 16 is dims 16 * db + 4 * g .. + 3
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb) {
+    const float sum = column_sum(w.l[cb]);
+    const int r = r0 + 16 * cb + mm;
+    if (r >= k.rows.count) continue;
+    int b, h, t;
+    k.rows.find(a, r, b, h, t);
+    const int z = k.rows.z;
+    const int64_t all_rows = (int64_t)a.Z * a.B * a.H * a.T, row = (((int64_t)z * a.B + b) * a.H + h) * a.T + t;
+    if (a.part_acc) {
+      float* p = a.part_acc + (k.slot * all_rows + row) * D + 4 * g;
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4*>(p + 16 * db) = w.o[cb][db];
+      if (g == 0) a.part_ml[k.slot * all_rows + row] = float2{w.m[cb], sum};
+    } else {
+      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+      E* o = static_cast<E*>(a.O) + z * a.os[0] + b * a.os[1] + h * a.os[2] + t * a.os[3] + 4 * g;
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) {
+        const f32x4 x = w.o[cb][db];
+        *reinterpret_cast<u32x2*>(o + 16 * db) = u32x2{pack2<E>(x[0] * inv, x[1] * inv), pack2<E>(x[2] * inv, x[3] * inv)};
+      }
+      if (a.lse && g == 0) a.lse[row] = natural_lse(w.m[cb], sum);
+    }
+  }
+}
+
+template <class E, int D, bool kWideS, bool kWideO>
+__global__ __launch_bounds__(kThreads, kWideS ? 2 : 3) void decode_kernel(const DecodeArgs a) {
+  const int tid = threadIdx.x;
+  // block id -> shared units (cache, KV head, part) x row blocks, then own units (.., sequence, part) x row blocks.  Row blocks of a unit
+  // read the same keys: they are given ids 8 apart, which land on one XCD at about the same time.
+  int id = blockIdx.x;
+  Block<E, D> k{a};
+  k.shared = id < a.ids_s;
+  const int blocks = k.shared ? a.blocks_s : a.blocks_o, units = k.shared ? a.units_s : a.units_o;
+  if (!k.shared) id -= a.ids_s;
+  const int turn = id / (8 * blocks);
+  id -= turn * 8 * blocks;
+  k.rb = id / 8;
+  int unit = turn * 8 + id % 8;
+  if (unit >= units) return;                       // an id that only rounds the grid up
+  k.rows.g = unit % a.Hkv;
+  unit /= a.Hkv;
+  if (k.shared) {
+    k.rows.b = -1;
+    k.rows.count = a.B * a.T * a.G;
+  } else {
+    k.rows.b = unit % a.B;
+    unit /= a.B;
+    k.rows.count = a.T * a.G;
+  }
+  k.rows.z = unit % a.Z;
+  k.part = unit / a.Z;
+  k.slot = k.shared ? k.part : a.splits_s + k.part;
+
+  constexpr int kTile = kKeys * D * 2, kWideTile = kWideKeys * D * 2;
+  __shared__ float2 ml[kWaves][16];
+  if constexpr (!kWideS && !kWideO) {
+    __shared__ __attribute__((aligned(256))) unsigned char smem[kWaves * kTile];
+    narrow_block(k, [&](int v) { return smem + v * kTile; }, ml, tid);
+  } else {
+    __shared__ __attribute__((aligned(256))) unsigned char ka[kWideTile], kb[kWideTile], va[kWideTile], vb[kWideTile];
+    if (kWideO || k.shared) wide_block(k, ka, kb, va, vb, tid);
+    else narrow_block(k, [&](int v) { return (v < 2 ? ka : kb) + (v & 1) * kTile; }, ml, tid);
   }
 }
 
@@ -327,7 +496,7 @@ template <class E, int D>
 __global__ __launch_bounds__(256) void decode_join_kernel(const DecodeArgs a, int parts, int lanes) {
   constexpr int kQuads = D / 4;
   __shared__ f32x4 acc_s[256];
-  __shared__ float sum_s[256];
+  __shared__ float2 ml_s[256];
   const int64_t all_rows = (int64_t)a.Z * a.B * a.H * a.T;
   const int per_row = kQuads * lanes, tid = threadIdx.x;
   const int64_t row = (int64_t)blockIdx.x * (256 / per_row) + tid / per_row;
@@ -336,26 +505,47 @@ __global__ __launch_bounds__(256) void decode_join_kernel(const DecodeArgs a, in
   float top = -INFINITY, sum = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   if (live) {
-    for (int p = 0; p < parts; ++p) top = fmaxf(top, a.part_ml[p * all_rows + row].x);
-#pragma unroll 4
-    for (int p = pl; p < parts; p += lanes) {
-      const float2 s = a.part_ml[p * all_rows + row];
-      const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_acc + (p * all_rows + row) * D + 4 * quad);
-      const float f = part_weight(s.x, top);
-      sum = fmaf(f, s.y, sum);
+    for (int p0 = pl; p0 < parts; p0 += 8 * lanes) {       // up to eight parts' loads in flight
+      float2 s[8];
+      f32x4 v[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] = fmaf(f, v[i], acc[i]);
+      for (int j = 0; j < 8; ++j) {
+        const int p = min(p0 + j * lanes, parts - 1);
+        s[j] = a.part_ml[p * all_rows + row];
+        v[j] = *reinterpret_cast<const f32x4*>(a.part_acc + (p * all_rows + row) * D + 4 * quad);
+      }
+      float next = top;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) next = fmaxf(next, s[j].x);
+      const float f0 = part_weight(top, next);
+      top = next;
+      sum *= f0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] *= f0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (p0 + j * lanes < parts) {
+          const float f = part_weight(s[j].x, top);
+          sum = fmaf(f, s[j].y, sum);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[i] = fmaf(f, v[j][i], acc[i]);
+        }
+      }
     }
   }
   if (lanes > 1) {
     acc_s[tid] = acc;
-    sum_s[tid] = sum;
+    ml_s[tid] = float2{top, sum};
     __syncthreads();
     if (pl != 0) return;
-    for (int p = 1; p < lanes; ++p) {
-      sum += sum_s[tid + p * kQuads];
+    for (int p = 1; p < lanes; ++p) top = fmaxf(top, ml_s[tid + p * kQuads].x);
+    sum = 0.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < lanes; ++p) {
+      const float f = part_weight(ml_s[tid + p * kQuads].x, top);
+      sum = fmaf(f, ml_s[tid + p * kQuads].y, sum);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] += acc_s[tid + p * kQuads][i];
+      for (int i = 0; i < 4; ++i) acc[i] = fmaf(f, acc_s[tid + p * kQuads][i], acc[i]);
     }
   }
   if (!live) return;
@@ -370,46 +560,53 @@ __global__ __launch_bounds__(256) void decode_join_kernel(const DecodeArgs a, in
   if (a.lse && quad == 0) a.lse[row] = natural_lse(top, sum);
 }
 
-constexpr int kWorkgroups = 768;   // that the split aims at: three on each of 256 CUs
-
 struct Shape {
-  int cb_s, blocks_s, splits_s, blocks_o, splits_o, direct;
+  bool wide_s, wide_o, direct;
+  int blocks_s, splits_s, blocks_o, splits_o;
   int parts() const { return splits_s + splits_o; }
 };
 
 // How the call's keys are dealt out.  (Host; a rule on the sizes the memory was laid out for, since the lengths may live on the device.)
 Shape shape_of(const DecodeArgs& a) {
   Shape s{};
-  const int64_t rows_s = (int64_t)a.B * a.T * a.G, rows_o = (int64_t)a.T * a.G;
-  const int64_t units = (int64_t)a.Z * a.Hkv;
-  s.blocks_s = (int)((rows_s + 15) / 16);
-  s.blocks_o = (int)((rows_o + 15) / 16);
-  const int64_t units_s = units * s.blocks_s, units_o = units * a.B * s.blocks_o;
-  s.direct = a.L + a.Lo <= 512 || (a.L == 0 && units_o >= kWorkgroups);
-  if (s.direct) {
+  const int64_t rows_o = (int64_t)a.T * a.G, rows_s = a.B * rows_o, heads = (int64_t)a.Z * a.Hkv;
+  // Few keys: a workgroup takes a sequence through both caches and nothing has to be joined.
+  s.direct = a.L == 0 || a.L + a.Lo <= 512;
+  s.wide_o = rows_o > kNarrowRows;
+  s.wide_s = s.wide_o || (rows_s > kNarrowRows && !s.direct);
+  const int rows_wg_s = s.wide_s ? kWideRows : kNarrowRows, rows_wg_o = s.wide_o ? kWideRows : kNarrowRows;
+  s.blocks_s = (int)((rows_s + rows_wg_s - 1) / rows_wg_s);
+  s.blocks_o = (int)((rows_o + rows_wg_o - 1) / rows_wg_o);
+  const int64_t units_s = heads * s.blocks_s, units_o = heads * a.B * s.blocks_o;
+  const int64_t slots = 256 * (s.wide_s ? 2 : 3);          // workgroups that are in flight together
+  if (s.direct && (a.L > 0 || units_o >= slots || a.Lo <= 512)) {
     s.splits_s = 0;
     s.splits_o = 1;
     return s;
   }
-  auto split = [](int64_t units, int64_t keys) {
-    const int64_t want = (kWorkgroups + units - 1) / units, most = (keys + 255) / 256;
-    return (int)(want < most ? want : most);
-  };
-  s.splits_s = a.L ? split(units_s, a.L) : 0;
-  s.splits_o = a.Lo ? split(units_o, a.Lo) : 0;
+  s.direct = false;
+  // One round of workgroups with the same number of keys each, 128 at least
+  const int64_t keys = (units_s * a.L + (a.Lo ? units_o * a.Lo : 0)) / slots;
+  auto split = [&](int64_t len) { return (int)(len == 0 ? 0 : len / (keys > 128 ? keys : 128) > 1 ? len / (keys > 128 ? keys : 128) : 1); };
+  s.splits_s = split(a.L);
+  s.splits_o = split(a.Lo);
   return s;
 }
 
 template <class E, int D>
 hipError_t launch(DecodeArgs a, const Shape& s, hipStream_t stream) {
   const int64_t all_rows = (int64_t)a.Z * a.B * a.H * a.T;
-  const int64_t units_s = (int64_t)a.Z * a.Hkv * s.blocks_s, units_o = (int64_t)a.Z * a.Hkv * a.B * s.blocks_o;
-  const int64_t blocks = units_s * s.splits_s + units_o * s.splits_o;
-  if (blocks <= 0 || blocks > 0x7fffffff) return hipErrorInvalidValue;
-  if (s.direct) a.part_acc = nullptr;
-  hipLaunchKernelGGL((decode_kernel<E, D, 1>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
+  const int64_t units_s = (int64_t)a.Z * a.Hkv * s.splits_s, units_o = (int64_t)a.Z * a.Hkv * a.B * s.splits_o;
+  const int64_t ids_s = (units_s + 7) / 8 * 8 * s.blocks_s, ids_o = (units_o + 7) / 8 * 8 * s.blocks_o;
+  if (ids_s + ids_o <= 0 || ids_s + ids_o > 0x7fffffff) return hipErrorInvalidValue;
+  a.units_s = (int)units_s; a.units_o = (int)units_o; a.ids_s = (int)ids_s;
+  if (s.parts() == 1) a.part_acc = nullptr;                // nothing to join
+  const dim3 grid((unsigned)(ids_s + ids_o)), threads(kThreads);
+  if (s.wide_o) hipLaunchKernelGGL((decode_kernel<E, D, true, true>), grid, threads, 0, stream, a);
+  else if (s.wide_s) hipLaunchKernelGGL((decode_kernel<E, D, true, false>), grid, threads, 0, stream, a);
+  else hipLaunchKernelGGL((decode_kernel<E, D, false, false>), grid, threads, 0, stream, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || s.direct) return e;
+  if (e != hipSuccess || !a.part_acc) return e;
   int lanes = 1;
   while (lanes < 1024 / D && lanes * 2 <= s.parts()) lanes *= 2;
   const int64_t per = 256 / (D / 4 * lanes);
@@ -421,7 +618,7 @@ hipError_t launch(DecodeArgs a, const Shape& s, hipStream_t stream) {
 
 size_t decode_scratch_bytes(const DecodeArgs& a) {
   const Shape s = shape_of(a);
-  if (s.direct) return 0;
+  if (s.parts() == 1) return 0;
   const size_t rows = (size_t)a.Z * a.B * a.H * a.T;
   return (size_t)s.parts() * rows * (a.D * 4 + 8);
 }

@@ -109,6 +109,7 @@ struct DecodeArgs {
   float* part_acc;
   float2* part_ml;
   int blocks_s, splits_s, blocks_o, splits_o, direct;
+  int units_s, units_o, ids_s;   // (cache, KV head, part) and (.., sequence, part); block ids of shared row blocks
 };
 size_t decode_scratch_bytes(const DecodeArgs& a);
 hipError_t launch_decode(DecodeArgs a, void* scratch, hipStream_t stream);
