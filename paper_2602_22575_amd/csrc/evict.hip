@@ -1,10 +1,14 @@
 // Eviction from a cache by accumulated attention weight, for gfx950: of n rows the first `sink`, the last `recent` and, of those
 // between, the ones of the largest weights stay (ties: the lowest index), in their order, moved together.
 //
-// Weights are ranked by an unsigned key that orders like the float (-0 as +0, NaN as -inf).  select_kernel finds, a
-// workgroup per (cache, KV head), the key of the last row that stays and how many rows of just that key do, by four rounds
-// of 8 bits; its wavefronts then count and list the rows of their own stretch of the cache.  gather_kernel copies the listed
-// rows of K and V.  Bound: HBM bandwidth of the copy; the selection reads the weights from L2 after the first round.
+// Weights are ranked by an unsigned key that orders like the float (-0 as +0, NaN as -inf).  What stays is the rows above the key of the
+// last one, and of those that share it the first few.
+//   select_kernel  up to 32K rows, a workgroup per (cache, KV head): all keys, and counts of 11, 11 and 10 of their bits, in LDS
+//   count_kernel, collect_kernel, list_kernel    more rows, a workgroup per stretch of 4096: count the keys' upper 11 bits; collect the
+//                  other 21 bits of the rows that share the last one's; settle them (every workgroup for itself, from LDS where they
+//                  fit) and list.  Three passes over the weights by all of the chip: one workgroup a head took 102 us
+//                  for 8 heads of 128K rows, bound by the instructions of one CU.
+// gather_kernel copies the listed rows of K and V and their weights.  Bound: HBM bandwidth of the copy.
 #include "cache_tile.h"
 #include "s2o_internal.h"
 
@@ -14,8 +18,6 @@ namespace {
 
 using namespace cache;
 
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
-
 // larger key = stays longer
 __device__ __forceinline__ uint32_t rank_key(float w) {
   if (w != w) w = -INFINITY;
@@ -23,133 +25,396 @@ __device__ __forceinline__ uint32_t rank_key(float w) {
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
-__global__ __launch_bounds__(kSelectThreads) void select_kernel(const EvictArgs a) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t found[2];                          // digit, rows above it
-  __shared__ int counts[kSelectWaves][2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t head = blockIdx.x;
-  const int z = (int)(head / a.Hkv);
-  const int n = filled(a.lens, z, a.L), stay = min(n, a.keep);
-  const float* w = a.weights + head * a.L;
-  if (a.lens_out && head % a.Hkv == 0 && tid == 0) a.lens_out[z] = stay;
-
-  // rows lo .. hi - 1 compete for `want` places
-  const int lo = min(a.sink, n), hi = max(lo, n - a.recent);
-  const int want = stay - (n - (hi - lo));
-  uint32_t key = 0;                                      // the last one's, found from the top digit down
-  int above = 0;                                         // rows with a larger key
-  if (want > 0 && want < hi - lo) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      for (int i = lo + tid; i < hi; i += kSelectThreads) {
-        const uint32_t k = rank_key(w[i]);
-        if (shift == 24 || (k >> (shift + 8)) == (key >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1u);
-      }
-      __syncthreads();
-      if (wave == 0) {                                   // suffix sums of 256 counts, 4 a lane, the largest digit first
-        uint32_t c[4], own = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { c[j] = hist[255 - (4 * lane + j)]; own += c[j]; }
-        uint32_t sum = own;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-          const uint32_t o = __shfl_up(sum, d);
-          if (lane >= d) sum += o;
-        }
-        uint32_t before = above + sum - own;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (before < (uint32_t)want && before + c[j] >= (uint32_t)want) {
-            found[0] = 255 - (4 * lane + j);
-            found[1] = before;
-          }
-          before += c[j];
-        }
-      }
-      __syncthreads();
-      key |= found[0] << shift;
-      above = (int)found[1];
-      __syncthreads();
-    }
+// The rows lo .. hi - 1 of n compete for `want` places, the others stay; `stay` in all.
+struct Places {
+  int n, stay, lo, hi, want;
+  __device__ __forceinline__ Places(const EvictArgs& a, int z) {
+    n = filled(a.lens, z, a.L);
+    stay = min(n, a.keep);
+    lo = min(a.sink, n);
+    hi = max(lo, n - a.recent);
+    want = stay - (n - (hi - lo));
   }
-  const bool all = want >= hi - lo;                      // every competing row stays
-  const int ties = want - above;                         // rows of exactly `key` that stay
+  __device__ __forceinline__ bool choose() const { return want > 0 && want < hi - lo; }   // else none of them stays, or all do
+};
 
-  // every wavefront lists its own stretch; what stands in front of it is counted first
-  const int per = ((n + kSelectWaves - 1) / kSelectWaves + 63) / 64 * 64;
-  const int from = min(wave * per, n), to = min(from + per, n);
-  auto classify = [&](int i, bool& sure, bool& tie) {
-    sure = tie = false;
-    if (i >= to) return;
-    if (i < lo || i >= hi || all) { sure = true; return; }
-    if (want <= 0) return;
-    const uint32_t k = rank_key(w[i]);
-    sure = k > key;
-    tie = k == key;
-  };
-  int sures = 0, tied = 0;
-  for (int i = from + lane; i - lane < to; i += 64) {
-    bool sure, tie;
-    classify(i, sure, tie);
-    sures += __popcll(__ballot(sure));
-    tied += __popcll(__ballot(tie));
-  }
-  if (lane == 0) { counts[wave][0] = sures; counts[wave][1] = tied; }
+constexpr int kT = 1024, kWaves = kT / 64;
+constexpr int kOneGroup = 32 * kT;  // rows that select_kernel takes
+constexpr int kBlock = 4 * kT;      // rows that a workgroup looks at at once, four in a row a thread
+constexpr int kStretches = 2048;    // of a row of weights at most: a stretch's number takes the 11 bits that an entry's key leaves
+constexpr int kBins = 2048;
+constexpr int kRoom = 16384;        // entries that list_kernel keeps in LDS
+
+// Sums over the lanes up to and with this one: 16 lanes by shifts, then the rows' last lanes passed on.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31 into rows 2 and 3
+  return x;
+}
+
+// Sums over the threads in front of this one, and over all, of two numbers.  `part`: a pair a wavefront.  (A barrier in front: `part` may be
+// in use.)
+struct Sums { int a, b, all_a, all_b; };
+__device__ __forceinline__ Sums block_scan(int a, int b, int2* part, int tid) {
+  const int sa = wave_scan(a), sb = wave_scan(b);
   __syncthreads();
-  int sure_before = 0, tie_before = 0;
-  for (int v = 0; v < wave; ++v) { sure_before += counts[v][0]; tie_before += counts[v][1]; }
-  const uint64_t below = (1ull << lane) - 1;
-  for (int i = from + lane; i - lane < to; i += 64) {
-    bool sure, tie;
-    classify(i, sure, tie);
-    const uint64_t sm = __ballot(sure), tm = __ballot(tie);
-    const int my_tie = tie_before + __popcll(tm & below), my_sure = sure_before + __popcll(sm & below);
-    if (sure || (tie && my_tie < ties)) {
-      const int64_t at = head * a.keep + my_sure + min(my_tie, ties);
-      a.kept[at] = i;
-      if (a.weights_out) a.weights_out[at] = w[i];
-    }
-    sure_before += __popcll(sm);
-    tie_before += __popcll(tm);
+  if ((tid & 63) == 63) part[tid >> 6] = int2{sa, sb};
+  __syncthreads();
+  Sums s{sa - a, sb - b, 0, 0};
+#pragma unroll
+  for (int v = 0; v < kWaves; ++v) {
+    const int2 x = part[v];
+    if (v < tid >> 6) { s.a += x.x; s.b += x.y; }
+    s.all_a += x.x;
+    s.all_b += x.y;
+  }
+  return s;
+}
+
+// counts[0 .. kBins - 1] -> the bin of the want-th largest (1 <= want <= the counts' sum), how many it holds, and how many lie in larger bins.
+struct Bin { int bin, holds, above; };
+__device__ __forceinline__ Bin find_bin(const uint32_t* counts, int2* part, Bin* found, int want, int tid) {
+  static_assert(kBins == 2 * kT, "two bins a thread");
+  const int b = kBins - 2 - 2 * tid;                       // the largest first
+  const uint2 c = *reinterpret_cast<const uint2*>(counts + b);
+  const int own = (int)(c.x + c.y), before = block_scan(own, 0, part, tid).a;
+  if (before < want && before + own >= want) {
+    const bool upper = before + (int)c.y >= want;
+    *found = upper ? Bin{b + 1, (int)c.y, before} : Bin{b, (int)c.x, before + (int)c.y};
+  }
+  __syncthreads();
+  return *found;
+}
+
+__host__ __device__ inline int stretch_rows(int L) { return (int)(((int64_t)L + (int64_t)kStretches * kBlock - 1) / ((int64_t)kStretches * kBlock)) * kBlock; }
+__host__ __device__ inline int stretches(int L) { return (L + stretch_rows(L) - 1) / stretch_rows(L); }
+
+// The scratch words of a head: counts, then what the kernels hand on, then entries.
+struct Scratch {
+  uint32_t* counts;    // [kBins] of the keys' upper 11 bits
+  uint32_t* known;     // [0]: those of the last row that stays, [1]: places for the rows that share them, [2]: entries
+  uint32_t* above;     // [stretches] rows of larger upper bits
+  uint32_t* entries;   // rows that share them: the other 21 bits, and the stretch
+  static constexpr int kHead = kBins + 64;
+  static __host__ __device__ size_t words(int L) { return kHead + (size_t)(stretches(L) + 63) / 64 * 64 + ((size_t)L + 63) / 64 * 64; }
+  __device__ __forceinline__ Scratch(const EvictArgs& a, int64_t head) {
+    counts = a.scratch + head * (int64_t)words(a.L);
+    known = counts + kBins;
+    above = counts + kHead;
+    entries = above + (stretches(a.L) + 63) / 64 * 64;
+  }
+};
+
+// Keys of four rows from row i on (behind the end: the last row's).  n > 0.  (Four loads without a branch rather than one with: several
+// calls' are in flight together.)
+__device__ __forceinline__ void four(const float* w, int i, int n, uint32_t (&k)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) k[e] = rank_key(w[min(i + e, n - 1)]);
+}
+
+// Lists rows of a thread: from + j for the bits j of `sure`, and of `tie` those that find a place.  s, t: such rows in front of the thread's.
+__device__ __forceinline__ void list_rows(int32_t* list, int from, uint64_t sure, uint64_t tie, int s, int t, int ties) {
+  uint64_t left = sure | tie;
+  while (left) {
+    const int j = __builtin_ctzll(left);
+    const int is_tie = (int)(tie >> j) & 1;
+    left &= left - 1;
+    if (!is_tie || t < ties) list[s + min(t, ties)] = from + j;
+    s += 1 - is_tie;
+    t += is_tie;
   }
 }
 
-// Rows of 2 * D bytes, D / 8 lanes a row; blockIdx.y: K or V.
-__global__ __launch_bounds__(256) void gather_kernel(const EvictArgs a, int lanes, int rows_block, int chunks) {
-  const int64_t head = blockIdx.x / chunks;
-  const int z = (int)(head / a.Hkv), hk = (int)(head % a.Hkv);
-  const int stay = min(filled(a.lens, z, a.L), a.keep);
-  const int row0 = (int)(blockIdx.x % chunks) * rows_block;
-  const int end = min(row0 + rows_block, stay);
-  const uint16_t* src = static_cast<const uint16_t*>(blockIdx.y ? a.V : a.K);
-  uint16_t* dst = static_cast<uint16_t*>(blockIdx.y ? a.V_out : a.K_out);
-  if (!src) return;
-  const int64_t* ss = blockIdx.y ? a.vs : a.ks;
-  const int64_t* ds = blockIdx.y ? a.vos : a.kos;
-  src += z * ss[0] + hk * ss[1] + 8 * (threadIdx.x % lanes);
-  dst += z * ds[0] + hk * ds[1] + 8 * (threadIdx.x % lanes);
+__global__ __launch_bounds__(256) void clear_kernel(const EvictArgs a) {
+  const Scratch s(a, blockIdx.x);
+  for (int i = threadIdx.x; i < Scratch::kHead; i += 256) s.counts[i] = 0;
+}
+
+__global__ __launch_bounds__(kT) void count_kernel(const EvictArgs a) {
+  __shared__ uint32_t counts[kBins];
+  const int tid = threadIdx.x;
+  const int stretch = (int)(blockIdx.x % stretches(a.L));
+  const int64_t head = blockIdx.x / stretches(a.L);
+  const Places p(a, (int)(head / a.Hkv));
+  const int per = stretch_rows(a.L), from = stretch * per, to = min(p.hi, from + per);
+  if (!p.choose() || from >= to) return;
+  for (int i = tid; i < kBins; i += kT) counts[i] = 0;
+  __syncthreads();
+  const float* w = a.weights + head * a.L;
+  for (int i = from + 4 * tid; i < to; i += kBlock) {
+    uint32_t k[4];
+    four(w, i, p.n, k);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (i + e >= p.lo && i + e < to) atomicAdd(&counts[k[e] >> 21], 1u);
+  }
+  __syncthreads();
+  const Scratch s(a, head);
+  for (int i = tid; i < kBins; i += kT)
+    if (counts[i]) atomicAdd(&s.counts[i], counts[i]);
+}
+
+__global__ __launch_bounds__(kT) void collect_kernel(const EvictArgs a) {
+  __shared__ int2 part[kWaves];
+  __shared__ Bin found;
+  __shared__ uint32_t base;
+  const int tid = threadIdx.x;
+  const int stretch = (int)(blockIdx.x % stretches(a.L));
+  const int64_t head = blockIdx.x / stretches(a.L);
+  const Places p(a, (int)(head / a.Hkv));
+  const int per = stretch_rows(a.L), from = stretch * per, to = min(p.hi, from + per);
+  if (!p.choose() || from >= p.n) return;
+  const Scratch s(a, head);
+  const Bin last = find_bin(s.counts, part, &found, p.want, tid);
+  if (stretch == 0 && tid == 0) {
+    s.known[0] = (uint32_t)last.bin;
+    s.known[1] = (uint32_t)(p.want - last.above);
+  }
+  const float* w = a.weights + head * a.L;
+  int above = 0;
+  for (int i0 = from; i0 < to; i0 += kBlock) {
+    const int i = i0 + 4 * tid;
+    uint32_t k[4];
+    four(w, i, p.n, k);
+    int mine = 0, larger = 0;
+    bool same[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool in = i + e >= p.lo && i + e < to;
+      larger += in && (int)(k[e] >> 21) > last.bin;
+      same[e] = in && (int)(k[e] >> 21) == last.bin;
+      mine += same[e];
+    }
+    // room for them.  (Entries are a set: their order does not matter.)
+    const Sums sums = block_scan(mine, larger, part, tid);
+    above += sums.all_b;
+    if (tid == 0) base = sums.all_a ? atomicAdd(&s.known[2], (uint32_t)sums.all_a) : 0u;
+    __syncthreads();
+    int at = (int)base + sums.a;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (same[e]) s.entries[at++] = (k[e] & 0x1fffffu) | (uint32_t)stretch << 21;
+  }
+  if (tid == 0) s.above[stretch] = (uint32_t)above;
+}
+
+__global__ __launch_bounds__(kT) void list_kernel(const EvictArgs a) {
+  __shared__ uint32_t counts[kBins], room[kRoom];
+  __shared__ int2 part[kWaves];
+  __shared__ Bin found;
+  const int tid = threadIdx.x;
+  const int stretch = (int)(blockIdx.x % stretches(a.L));
+  const int64_t head = blockIdx.x / stretches(a.L);
+  const Places p(a, (int)(head / a.Hkv));
+  const int per = stretch_rows(a.L), from = stretch * per, to = min(p.n, from + per);
+  if (a.lens_out && stretch == 0 && head % a.Hkv == 0 && tid == 0) a.lens_out[head / a.Hkv] = p.stay;
+  if (from >= to) return;
+  const Scratch s(a, head);
+  const bool choose = p.choose(), all = !choose && p.want > 0;
+  uint32_t key = 0;
+  int ties = 0, kept_before = all ? from : min(p.lo, from) + max(0, from - p.hi), tied_before = 0;
+  if (choose) {
+    const int used = (int)s.known[2], here = min(used, kRoom);
+    key = s.known[0] << 21;
+    ties = (int)s.known[1];
+    int kept = 0, tied = 0;
+    for (int i = tid; i < stretch; i += kT) kept += (int)s.above[i];
 #pragma unroll 4
-  for (int r = row0 + threadIdx.x / lanes; r < end; r += 256 / lanes) {
-    const int from = a.kept[head * a.keep + r];
-    *reinterpret_cast<u32x4*>(dst + r * ds[2]) = *reinterpret_cast<const u32x4*>(src + from * ss[2]);
+    for (int i = tid; i < here; i += kT) room[i] = s.entries[i];
+    auto each = [&](auto f) {
+#pragma unroll 1
+      for (int i = tid; i < here; i += kT) f(room[i]);
+#pragma unroll 1
+      for (int i = kRoom + tid; i < used; i += kT) f(s.entries[i]);
+    };
+    // 11 and 10 bits more
+#pragma unroll 1
+    for (int shift = 10; shift >= 0; shift -= 10) {
+      const uint32_t known = shift == 10 ? 21 : 10, mask = shift == 10 ? 2047 : 1023;
+      __syncthreads();
+      for (int i = tid; i < kBins; i += kT) counts[i] = 0;
+      __syncthreads();
+      each([&](uint32_t x) {
+        const uint32_t k = x & 0x1fffffu;
+        if ((k >> known) == ((key & 0x1fffffu) >> known)) atomicAdd(&counts[(k >> shift) & mask], 1u);
+      });
+      __syncthreads();
+      const Bin last = find_bin(counts, part, &found, ties, tid);
+      key |= (uint32_t)last.bin << shift;
+      ties -= last.above;
+    }
+    // what stays in front of this stretch, for certain and if there are places
+    each([&](uint32_t x) {
+      const uint32_t k = x & 0x1fffffu, last = key & 0x1fffffu;
+      const bool front = (int)(x >> 21) < stretch;
+      kept += front && k > last;
+      tied += front && k == last;
+    });
+    const Sums sums = block_scan(kept, tied, part, tid);
+    kept_before += sums.all_a;
+    tied_before = sums.all_b;
+  }
+  const float* w = a.weights + head * a.L;
+  for (int i0 = from; i0 < to; i0 += kBlock) {
+    const int i = i0 + 4 * tid;
+    uint32_t k[4], sure = 0, tie = 0;
+    four(w, i, p.n, k);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool competes = i + e >= p.lo && i + e < p.hi;
+      if (i + e < to && (!competes || all || (choose && k[e] > key))) sure |= 1u << e;
+      if (i + e < to && competes && choose && k[e] == key) tie |= 1u << e;
+    }
+    const Sums sums = block_scan(__popc(sure), __popc(tie), part, tid);
+    list_rows(a.kept + head * a.keep, i, sure, tie, kept_before + sums.a, tied_before + sums.b, ties);
+    kept_before += sums.all_a;
+    tied_before += sums.all_b;
+  }
+}
+
+// kRows: of a head at most.
+template <int kRows>
+__global__ __launch_bounds__(kT) void select_kernel(const EvictArgs a) {
+  __shared__ __attribute__((aligned(16))) uint32_t keys[kRows];   // 0: a row that does not compete (the least key is 0x7fffff)
+  __shared__ uint32_t counts[kBins];
+  __shared__ int2 part[kWaves];
+  __shared__ Bin found;
+  const int tid = threadIdx.x;
+  const int64_t head = blockIdx.x;
+  const Places p(a, (int)(head / a.Hkv));
+  if (a.lens_out && head % a.Hkv == 0 && tid == 0) a.lens_out[head / a.Hkv] = p.stay;
+  if (p.n == 0) return;
+  const float* w = a.weights + head * a.L;
+  const bool choose = p.choose(), all = !choose && p.want > 0;
+  for (int i = tid; i < kBins; i += kT) counts[i] = 0;
+  __syncthreads();
+#pragma unroll 4
+  for (int i = 4 * tid; i < p.n; i += kBlock) {
+    uint32_t k[4];
+    four(w, i, p.n, k);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (i + e < p.lo || i + e >= p.hi) k[e] = 0;
+      if (k[e] && choose) atomicAdd(&counts[k[e] >> 21], 1u);
+    }
+    *reinterpret_cast<u32x4*>(keys + i) = u32x4{k[0], k[1], k[2], k[3]};
+  }
+  __syncthreads();
+  // From here on a thread has a stretch of its own: an odd number of pieces of four rows, so that a wavefront's reads meet different banks.
+  const int per = 4 * (((p.n + kBlock - 1) / kBlock) | 1), from = min(tid * per, p.n), to = min(from + per, p.n);
+  uint32_t key = 0, known = 0;                             // what is known of the last row's key, from the top down
+  int ties = p.want;                                       // places for the rows that share it
+  if (choose) {
+#pragma unroll 1
+    for (int shift = 21; ; shift = shift == 21 ? 10 : 0) {
+      const uint32_t mask = shift == 0 ? 1023 : 2047;
+      if (shift != 21) {
+        for (int i = tid; i < kBins; i += kT) counts[i] = 0;
+        __syncthreads();
+#pragma unroll 1
+        for (int i = from; i < to; i += 4) {
+          const u32x4 k = *reinterpret_cast<const u32x4*>(keys + i);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (i + e < to && k[e] && (k[e] & known) == key) atomicAdd(&counts[(k[e] >> shift) & mask], 1u);
+        }
+        __syncthreads();
+      }
+      const Bin last = find_bin(counts, part, &found, ties, tid);
+      key |= (uint32_t)last.bin << shift;
+      known |= mask << shift;
+      ties -= last.above;
+      if (last.holds == ties || shift == 0) break;         // (all that share it stay)
+      __syncthreads();
+    }
+  }
+  static_assert(4 * ((kRows / kBlock) | 1) <= 64, "a thread's rows are the bits of a word");
+  uint64_t sure = 0, tie = 0;
+#pragma unroll 1
+  for (int i = from; i < to; i += 4) {
+    const u32x4 k = *reinterpret_cast<const u32x4*>(keys + i);
+    uint32_t s4 = 0, t4 = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (i + e < to && (k[e] == 0 || all || (choose && (k[e] & known) > key))) s4 |= 1u << e;
+      if (i + e < to && k[e] != 0 && choose && (k[e] & known) == key) t4 |= 1u << e;
+    }
+    sure |= (uint64_t)s4 << (i - from);
+    tie |= (uint64_t)t4 << (i - from);
+  }
+  const Sums sums = block_scan(__popcll(sure), __popcll(tie), part, tid);
+  list_rows(a.kept + head * a.keep, from, sure, tie, sums.a, sums.b, ties);
+}
+
+// Rows of 2 * D bytes, D / 8 lanes a row, kEach of them a thread; blockIdx.y: K and the weights, or V.
+template <int D, int kEach>
+__global__ __launch_bounds__(256) void gather_kernel(const EvictArgs a, int chunks) {
+  constexpr int kLanes = D / 8, kStep = 256 / kLanes;
+  const int64_t head = blockIdx.x / chunks;
+  const int z = (int)(head / a.Hkv), hk = (int)(head % a.Hkv), lane = threadIdx.x % kLanes;
+  const int stay = min(filled(a.lens, z, a.L), a.keep);
+  const int r0 = (int)(blockIdx.x % chunks) * (kStep * kEach) + threadIdx.x / kLanes;
+  if (r0 >= stay) return;
+  int from[kEach];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) from[j] = a.kept[head * a.keep + min(r0 + kStep * j, stay - 1)];
+  const uint16_t* src = static_cast<const uint16_t*>(blockIdx.y ? a.V : a.K);
+  if (src) {
+    uint16_t* dst = static_cast<uint16_t*>(blockIdx.y ? a.V_out : a.K_out);
+    const int64_t* ss = blockIdx.y ? a.vs : a.ks;
+    const int64_t* ds = blockIdx.y ? a.vos : a.kos;
+    src += z * ss[0] + hk * ss[1] + 8 * lane;
+    dst += z * ds[0] + hk * ds[1] + 8 * lane;
+    u32x4 x[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) x[j] = *reinterpret_cast<const u32x4*>(src + from[j] * ss[2]);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+      if (r0 + kStep * j < stay) *reinterpret_cast<u32x4*>(dst + (r0 + kStep * j) * ds[2]) = x[j];
+  }
+  if (blockIdx.y == 0 && a.weights_out && lane < kEach) {
+    int mine = from[0];
+#pragma unroll
+    for (int j = 1; j < kEach; ++j) mine = lane == j ? from[j] : mine;
+    if (r0 + kStep * lane < stay) a.weights_out[head * a.keep + r0 + kStep * lane] = a.weights[head * a.L + mine];
   }
 }
 
 }  // namespace
 
-size_t evict_scratch_bytes(const EvictArgs&) { return 0; }
+size_t evict_scratch_bytes(const EvictArgs& a) {
+  return a.L <= kOneGroup ? 0 : (size_t)a.Z * a.Hkv * Scratch::words(a.L) * 4;
+}
 
-hipError_t launch_evict(const EvictArgs& a, void*, hipStream_t stream) {
+hipError_t launch_evict(EvictArgs a, void* scratch, hipStream_t stream) {
   const int64_t heads = (int64_t)a.Z * a.Hkv;
   if (heads > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(select_kernel, dim3((unsigned)heads), dim3(kSelectThreads), 0, stream, a);
+  if (a.L <= kOneGroup) {
+    const dim3 grid((unsigned)heads);
+    if (a.L <= 4 * kT) hipLaunchKernelGGL(select_kernel<4 * kT>, grid, dim3(kT), 0, stream, a);
+    else hipLaunchKernelGGL(select_kernel<kOneGroup>, grid, dim3(kT), 0, stream, a);
+  } else {
+    a.scratch = static_cast<uint32_t*>(scratch);
+    const int64_t blocks = heads * stretches(a.L);
+    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)blocks);
+    hipLaunchKernelGGL(clear_kernel, dim3((unsigned)heads), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(count_kernel, grid, dim3(kT), 0, stream, a);
+    hipLaunchKernelGGL(collect_kernel, grid, dim3(kT), 0, stream, a);
+    hipLaunchKernelGGL(list_kernel, grid, dim3(kT), 0, stream, a);
+  }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || (!a.K && !a.V)) return e;
-  const int lanes = a.D / 8, rows_block = 4 * (256 / lanes), chunks = (a.keep + rows_block - 1) / rows_block;
+  if (e != hipSuccess || (!a.K && !a.V && !a.weights_out)) return e;
+  constexpr int kEach = 4;
+  const int rows = 2048 / a.D * kEach, chunks = (a.keep + rows - 1) / rows;
   if (heads * chunks > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(gather_kernel, dim3((unsigned)(heads * chunks), 2), dim3(256), 0, stream, a, lanes, rows_block, chunks);
+  const dim3 grid((unsigned)(heads * chunks), a.V ? 2 : 1);
+  if (a.D == 128) hipLaunchKernelGGL((gather_kernel<128, kEach>), grid, dim3(256), 0, stream, a, chunks);
+  else hipLaunchKernelGGL((gather_kernel<64, kEach>), grid, dim3(256), 0, stream, a, chunks);
   return hipGetLastError();
 }
 

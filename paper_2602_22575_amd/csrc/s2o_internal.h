@@ -142,8 +142,9 @@ struct EvictArgs {
   int32_t *kept, *lens_out;
   int Z, Hkv, D, L, keep, sink, recent;
   int64_t ks[3], vs[3], kos[3], vos[3];
+  uint32_t* scratch;     // set by the launch
 };
 size_t evict_scratch_bytes(const EvictArgs& a);
-hipError_t launch_evict(const EvictArgs& a, void* scratch, hipStream_t stream);
+hipError_t launch_evict(EvictArgs a, void* scratch, hipStream_t stream);
 
 }  // namespace s2o
