@@ -3,12 +3,12 @@
 //   w[j] = prev[j] + sum_r exp(x_rj - lse_r),   x_rj = scale <q_r, k_j>,   r over the B*T*G rows of a (cache, KV head) that see j
 //
 // With the rows' lse given (of a softmax over more than these keys) one pass over the scores is enough; without it the
-// rows' softmax over the keys they see comes first, in a pass of its own.  Both passes form scores with MFMAs and keep one side of the product in
-// registers while 64-row tiles of the other stream through LDS, shared by the workgroup's four wavefronts:
-//   stats_kernel   64 query rows a wavefront as columns, key tiles stream: a lane keeps its own maximum and sum of its columns
-//                  over the keys it meets, lanes are joined once at the end;
-//   sum_kernel     64 keys a wavefront as columns, query tiles stream: a lane keeps one sum per key and nothing is
-//                  exchanged until the end.  A key's sum is made in one order by one workgroup: no atomics, the same bits every time.
+// rows' softmax over the keys they see comes first, in a pass of its own.  Both passes form scores with MFMAs, hold 64 query rows a wavefront in
+// registers and stream tiles of 64 keys through LDS, shared by the workgroup's four wavefronts:
+//   stats_kernel   query rows are the columns: a lane keeps its own maximum and sum of its rows over the keys it meets, lanes are
+//                  joined once at the end;
+//   sum_kernel     keys are the columns: a lane adds up a key's terms over the rows in its registers.  Every sum is made in one order: no
+//                  atomics, the same bits every time.
 // Rows are counted r = (t * B + b) * G + g, so that what a key is seen by is one range of rows.
 //
 // Statistics are kept as a base-2 reference m and 1/l instead of one lse: rounding m + log2 l would cost the weights
@@ -23,8 +23,9 @@ namespace {
 using namespace cache;
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kTileRows = 64;
-constexpr int kCols = 64;                          // columns of a wavefront: four blocks of 16
+constexpr int kCols = 64;                          // query rows of a wavefront: four blocks of 16
 constexpr int kColsWg = kCols * kWaves;
+constexpr int kRange = 32;                         // tiles of keys of a workgroup of sum_kernel at most
 
 struct RowOf {
   int t, b, g;
@@ -36,122 +37,186 @@ struct RowOf {
   }
 };
 
-// A tile of 64 rows on its way to LDS: D/32 pieces of 16 bytes a thread, row (D/8 lanes each) tid / (D/8) + i * rows a pass.
+// Keys that query token t sees.
+__device__ __forceinline__ int row_limit(const WeightsArgs& a, int len, int t) { return a.causal ? min(max(len - a.T + t + 1, 0), len) : len; }
+
+// The order of a tile's instructions: the products of a block of 16 keys one by one, behind each its share of the three instructions a score that the
+// block before it takes.  (Left to itself the compiler waits for one block's results and then works on them.)
 template <int D>
-struct Staged {
-  static constexpr int kLanes = D / 8, kPerPass = kThreads / kLanes, kPasses = kTileRows / kPerPass;
-  u32x4 x[kPasses];
-  __device__ __forceinline__ void store(unsigned char* tile, int tid) const {
+__device__ __forceinline__ void order_tile() {
+  constexpr int kProducts = D / 8, kVector = 48 / kProducts, kReads = D / 32;
+  __builtin_amdgcn_sched_group_barrier(0x100, 2 * kReads, 0);      // LDS reads
+  __builtin_amdgcn_sched_group_barrier(0x8, kProducts, 0);         // MFMA
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) *reinterpret_cast<u32x4*>(tile + at<D>(kPerPass * i + tid / kLanes, tid % kLanes)) = x[i];
+  for (int kb = 0; kb < 3; ++kb)
+#pragma unroll
+    for (int j = 0; j < kProducts; ++j) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, kVector, 0);     // VALU, transcendental
+      if (kb < 2 && j % 4 == 3) __builtin_amdgcn_sched_group_barrier(0x100, kReads / (kProducts / 4), 0);
+    }
+  __builtin_amdgcn_sched_group_barrier(0x402, 48, 0);
+}
+
+// Streams tiles from .. to - 1 of 64 keys through four LDS buffers, three tiles ahead of the one that is worked on: two workgroups a CU
+// then have 96 KB on their way (with one tile ahead the kernels waited for memory: 81 and 84 us for 128K keys of 8 heads).  All threads of
+// the workgroup; fast(t, tile) or, where it returns false, any(t, tile) works on tile t; the buffers are separate arrays, so
+// that the compiler sees that reads of one need not wait for the loads that fill another.
+template <class E, int D, class F, class G>
+__device__ __forceinline__ void stream_keys(const E* K, int64_t stride, int len, int from, int to, unsigned char* b0, unsigned char* b1,
+                                            unsigned char* b2, int tid, F fast, G any) {
+  constexpr int kLanes = D / 8, kRowsPerLoad = 64 / kLanes, kLoads = 16 / kRowsPerLoad;   // a wavefront loads 16 rows
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane / kLanes;
+  // LDS takes a load's lanes in order: each fetches the chunk that belongs at its slot
+  const uint32_t chunk = 16 * ((lane % kLanes) ^ swz<D>(lr)), row = (uint32_t)(stride * 2), off = (uint32_t)lr * row;
+  auto issue = [&](int t, unsigned char* tile) {
+    const auto keys = rows_buffer(K, stride * 2, t * kTileRows, len, kTileRows, 2 * D);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = 16 * wave + kRowsPerLoad * i;
+      buffer_load_to_lds(keys, off + r * row + (chunk ^ (swz<D>(kRowsPerLoad * i) << 4)), tile + r * 2 * D);
+    }
+  };
+  if (from >= to) return;
+  issue(from, b0);
+  if (from + 1 < to) issue(from + 1, b1);
+  auto step = [&](int t, unsigned char* tile, unsigned char* ahead) {
+    // what this wavefront fetched of tile t has landed (loads complete in order), and what it read of tile t - 1 is in its registers
+    asm volatile("" ::: "memory");
+    if (t + 1 < to) __builtin_amdgcn_s_waitcnt(0x0070 | kLoads);   // vmcnt(kLoads) lgkmcnt(0)
+    else __builtin_amdgcn_s_waitcnt(0x0070);
+    asm volatile("s_barrier" ::: "memory");
+    if (t + 2 < to) issue(t + 2, ahead);
+    if (!fast(t, tile)) any(t, tile);
+  };
+  for (int t = from;;) {
+    step(t, b0, b2);
+    if (++t >= to) break;
+    step(t, b1, b0);
+    if (++t >= to) break;
+    step(t, b2, b1);
+    if (++t >= to) break;
+  }
+}
+
+// ---- rows' softmax statistics over the keys they see
+//
+// A column's reference is the largest of the first scores that the lane meets: never above the true maximum, so that nothing
+// is lost below it, and 32-bit sums have room for 2^90 times as much above it.  So only a tile with hidden keys, the first one, and one after
+// which a sum has outgrown that look for the maximum; the others are products, exponentials and additions.
+constexpr float kRoomAbove = 0x1p90f;
+
+template <class E, int D>
+struct Stats {
+  typedef typename Vec<E>::x8 x8;
+  x8 q[4][D / 32];
+  int lim[4];
+  float m[4], l[4];              // reference (base 2), the lane's part of the sum
+
+  __device__ __forceinline__ void scores(const unsigned char* tile, int kb, f32x4 (&s)[4], int mm, int g) const {
+    x8 k[D / 32];
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) k[kk] = *reinterpret_cast<const x8*>(tile + 16 * kb * 2 * D + (at<D>(mm, g) ^ (kk << 6)));
+#pragma unroll
+    for (int cb = 0; cb < 4; ++cb) s[cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk)
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb) s[cb] = mfma(k[kk], q[cb][kk], s[cb]);
+  }
+  // All 64 keys seen, against the references as they are.  Exponentials of a block of 16 keys stand behind the products of the next one.
+  __device__ __forceinline__ bool tile_fast(const unsigned char* tile, float c2, int mm, int g) {
+    f32x4 s[2][4];
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    scores(tile, 0, s[0], mm, g);
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+      if (kb < 3) scores(tile, kb + 1, s[(kb + 1) & 1], mm, g);
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[cb] += exp2_(fmaf(s[kb & 1][cb][i], c2, -m[cb]));
+    }
+    order_tile<D>();
+    bool fits = true;
+#pragma unroll
+    for (int cb = 0; cb < 4; ++cb) fits &= l[cb] + sum[cb] <= kRoomAbove;    // (false for NaN)
+    if (__builtin_amdgcn_ballot_w64(!fits) != 0) return false;
+#pragma unroll
+    for (int cb = 0; cb < 4; ++cb) l[cb] += sum[cb];
+    return true;
+  }
+  __device__ __forceinline__ void tile_any(const unsigned char* tile, int key0, float c2, int mm, int g) {
+#pragma unroll 1
+    for (int kb = 0; kb < 4; ++kb) {
+      f32x4 s[4];
+      scores(tile, kb, s, mm, g);
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (key0 + 16 * kb + 4 * g + i >= lim[cb]) s[cb][i] = -INFINITY;
+          top = fmaxf(top, s[cb][i]);
+        }
+        const float m_new = fmaxf(m[cb], top * c2), ref = m_new == -INFINITY ? 0.f : m_new;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += exp2_(fmaf(s[cb][i], c2, -ref));
+        l[cb] = fmaf(l[cb], exp2_(m[cb] - ref), sum);
+        m[cb] = m_new;
+      }
+    }
   }
 };
 
-// ---- rows' softmax statistics over the keys they see
 template <class E, int D>
-__global__ __launch_bounds__(kThreads, 2) void stats_kernel(const WeightsArgs a) {
-  typedef typename Vec<E>::x8 x8;
+__global__ __launch_bounds__(kThreads, 3) void stats_kernel(const WeightsArgs a) {
   constexpr int kTile = kTileRows * D * 2;
-  __shared__ __attribute__((aligned(256))) unsigned char smem[2 * kTile];
+  __shared__ __attribute__((aligned(256))) unsigned char b0[kTile], b1[kTile], b2[kTile];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int mm = lane & 15, g = lane >> 4;
+  // the row blocks that see the most keys first
   int id = blockIdx.x;
-  const int rb = id % a.row_blocks;
-  id /= a.row_blocks;
   const int hk = id % a.Hkv;
   id /= a.Hkv;
-  const int z = id % a.Z, part = id / a.Z;
+  const int z = id % a.Z;
+  id /= a.Z;
+  const int part = id % a.key_parts, rb = a.row_blocks - 1 - id / a.key_parts;
   const int R = a.B * a.T * a.G, len = filled(a.lens, z, a.L);
   const E* Q = static_cast<const E*>(a.Q) + z * a.qs[0];
   const E* K = static_cast<const E*>(a.K) + z * a.ks[0] + hk * a.ks[1];
 
-  x8 q[4][D / 32];
-  int lim[4];
-  float m[4], l[4];
+  Stats<E, D> w;
 #pragma unroll
   for (int cb = 0; cb < 4; ++cb) {
     RowOf row;
     row.set(a, min(rb * kColsWg + wave * kCols + 16 * cb + mm, R - 1));
     const E* p = Q + row.b * a.qs[1] + (hk * a.G + row.g) * a.qs[2] + row.t * a.qs[3];
 #pragma unroll
-    for (int kk = 0; kk < D / 32; ++kk) q[cb][kk] = *reinterpret_cast<const x8*>(p + 32 * kk + 8 * g);
-    lim[cb] = a.causal ? min(max(len - a.T + row.t + 1, 0), len) : len;
-    m[cb] = -INFINITY;
-    l[cb] = 0.f;
+    for (int kk = 0; kk < D / 32; ++kk) w.q[cb][kk] = *reinterpret_cast<const typename Vec<E>::x8*>(p + 32 * kk + 8 * g);
+    w.lim[cb] = row_limit(a, len, row.t);
+    w.m[cb] = -INFINITY;
+    w.l[cb] = 0.f;
   }
-  // keys that the workgroup's last row sees
-  RowOf last;
-  last.set(a, min((rb + 1) * kColsWg, R) - 1);
-  const int seen = a.causal ? min(max(len - a.T + last.t + 1, 0), len) : len;
-  const int tiles = (seen + kTileRows - 1) / kTileRows;
+  // keys that the workgroup's first and last row see
+  RowOf row;
+  row.set(a, rb * kColsWg);
+  const int full = row_limit(a, len, row.t) / kTileRows;
+  row.set(a, min((rb + 1) * kColsWg, R) - 1);
+  const int tiles = (row_limit(a, len, row.t) + kTileRows - 1) / kTileRows;
   const int from = (int)((int64_t)tiles * part / a.key_parts), to = (int)((int64_t)tiles * (part + 1) / a.key_parts);
+  const bool active = rb * kColsWg + wave * kCols < R;     // the wavefront has rows at all
 
-  Staged<D> st;
-  const uint32_t krow = (uint32_t)(a.ks[2] * 2);
-  auto load = [&](int t) {
-    const char* base = reinterpret_cast<const char*>(K + (int64_t)t * kTileRows * a.ks[2]);
-    const int most = len - 1 - t * kTileRows;
-#pragma unroll
-    for (int i = 0; i < st.kPasses; ++i) {
-      const uint32_t off = (uint32_t)min(st.kPerPass * i + tid / st.kLanes, most) * krow + 16 * (tid % st.kLanes);
-      st.x[i] = *reinterpret_cast<const u32x4*>(base + off);
-    }
-  };
-  if (from < to) load(from);
-  for (int t = from; t < to; ++t) {
-    unsigned char* tile = smem + ((t - from) & 1) * kTile;
-    st.store(tile, tid);
-    __syncthreads();
-    if (t + 1 < to) load(t + 1);
-    f32x4 s[4][4];                                 // [16-key block][column block]
-#pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
-      x8 k[D / 32];
-#pragma unroll
-      for (int kk = 0; kk < D / 32; ++kk) k[kk] = *reinterpret_cast<const x8*>(tile + at<D>(16 * kb + mm, 4 * kk + g));
-#pragma unroll
-      for (int cb = 0; cb < 4; ++cb) {
-        s[kb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kk = 0; kk < D / 32; ++kk) s[kb][cb] = mfma(k[kk], q[cb][kk], s[kb][cb]);
-      }
-    }
-    const int key0 = t * kTileRows;
-    bool hidden = false;
-#pragma unroll
-    for (int cb = 0; cb < 4; ++cb) hidden |= lim[cb] < key0 + kTileRows;
-    if (__builtin_amdgcn_ballot_w64(hidden) != 0) {
-#pragma unroll
-      for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-        for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (key0 + 16 * kb + 4 * g + i >= lim[cb]) s[kb][cb][i] = -INFINITY;
-    }
-#pragma unroll
-    for (int cb = 0; cb < 4; ++cb) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[kb][cb][i]);
-      const float m_new = fmaxf(m[cb], top * a.c2), ref = m_new == -INFINITY ? 0.f : m_new;
-      float sum = 0.f;
-#pragma unroll
-      for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum += exp2_(fmaf(s[kb][cb][i], a.c2, -ref));
-      l[cb] = fmaf(l[cb], exp2_(m[cb] - ref), sum);
-      m[cb] = m_new;
-    }
-  }
+  stream_keys<E, D>(K, a.ks[2], len, from, to, b0, b1, b2, tid,
+                    [&](int t, const unsigned char* tile) { return !active || (t > from && t < full && w.tile_fast(tile, a.c2, mm, g)); },
+                    [&](int t, const unsigned char* tile) { w.tile_any(tile, t * kTileRows, a.c2, mm, g); });
   // join the four lanes of a column
   const int64_t rows = (int64_t)a.Z * a.Hkv * R;
 #pragma unroll
   for (int cb = 0; cb < 4; ++cb) {
-    const float top = column_max(m[cb]), ref = top == -INFINITY ? 0.f : top;
-    const float sum = column_sum(l[cb] * exp2_(m[cb] - ref));
+    const float top = column_max(w.m[cb]), ref = top == -INFINITY ? 0.f : top;
+    const float sum = column_sum(w.l[cb] * exp2_(w.m[cb] - ref));
     const int r = rb * kColsWg + wave * kCols + 16 * cb + mm;
     if (g == 0 && r < R) {
       const int64_t i = ((int64_t)z * a.Hkv + hk) * R + r;
@@ -161,145 +226,184 @@ __global__ __launch_bounds__(kThreads, 2) void stats_kernel(const WeightsArgs a)
   }
 }
 
+// Sixteen rows a workgroup, sixteen lanes a row.
 __global__ __launch_bounds__(256) void stats_join_kernel(float2* stats, int64_t rows, int parts) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= rows) return;
+  const int64_t i = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+  const int lane = threadIdx.x % 16;
   float top = -INFINITY, sum = 0.f;
-  for (int p = 0; p < parts; ++p) top = fmaxf(top, stats[p * rows + i].x);
-  const float ref = top == -INFINITY ? 0.f : top;
-  for (int p = 0; p < parts; ++p) {
-    const float2 s = stats[p * rows + i];
-    sum = fmaf(exp2_(s.x - ref), s.y, sum);
+  if (i < rows) {
+#pragma unroll 4
+    for (int p = lane; p < parts; p += 16) {
+      const float2 s = stats[p * rows + i];
+      const float next = fmaxf(top, s.x), ref = next == -INFINITY ? 0.f : next;
+      sum = fmaf(sum, exp2_(top - ref), s.y * exp2_(s.x - ref));
+      top = next;
+    }
   }
-  stats[i] = sum == 0.f ? float2{INFINITY, 0.f} : float2{ref, 1.0f / sum};
+  float all = top;
+#pragma unroll
+  for (int d = 1; d < 16; d *= 2) all = fmaxf(all, __shfl_xor(all, d));
+  const float ref = all == -INFINITY ? 0.f : all;
+  sum *= exp2_(top - ref);
+#pragma unroll
+  for (int d = 1; d < 16; d *= 2) sum += __shfl_xor(sum, d);
+  if (i < rows && lane == 0) stats[i] = sum == 0.f ? float2{INFINITY, 0.f} : float2{ref, 1.0f / sum};
 }
 
 // ---- the weights
+//
+// A workgroup has a range of up to kRange tiles of keys and some of the row blocks.  Per row block its wavefronts hold 64 rows each, this time as the
+// A side, so that a lane of an accumulator block is a key and its registers are rows: a key's terms are added up inside the lane.  A tile's sums of the four
+// wavefronts meet in LDS and add to the range's.
 template <class E, int D, bool kGiven>
 __global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs a) {
   typedef typename Vec<E>::x8 x8;
   constexpr int kTile = kTileRows * D * 2;
-  __shared__ __attribute__((aligned(256))) unsigned char smem[2 * kTile];
-  __shared__ __attribute__((aligned(16))) float ref_s[2][kTileRows], inv_s[2][kTileRows];
-  __shared__ __attribute__((aligned(16))) int lim_s[2][kTileRows];
+  __shared__ __attribute__((aligned(256))) unsigned char b0[kTile], b1[kTile], b2[kTile];
+  __shared__ float range_s[kRange * kTileRows], tile_s[2][kWaves][kTileRows];
+  __shared__ __attribute__((aligned(16))) float ref_s[kWaves][kCols], inv_s[kWaves][kCols];
+  __shared__ __attribute__((aligned(16))) int lim_s[kWaves][kCols];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int mm = lane & 15, g = lane >> 4;
+  // the ranges and the row blocks with the most work first: the first keys, the last rows
   int id = blockIdx.x;
   const int hk = id % a.Hkv;
   id /= a.Hkv;
   const int z = id % a.Z;
   id /= a.Z;
-  const int part = id % a.row_parts, kblock = id / a.row_parts;
+  const int part = a.row_parts - 1 - id % a.row_parts, range = id / a.row_parts;
   const int R = a.B * a.T * a.G, len = filled(a.lens, z, a.L);
-  const int key0 = kblock * kColsWg;
-  if (key0 >= len) return;                         // (uniform: rows behind the cache's end stay as they are)
+  const int t0 = range * a.range_tiles, t1 = min(t0 + a.range_tiles, (len + kTileRows - 1) / kTileRows);
+  if (t0 >= t1) return;                            // (uniform: entries behind the cache's end stay as they are)
   const E* Q = static_cast<const E*>(a.Q) + z * a.qs[0];
   const E* K = static_cast<const E*>(a.K) + z * a.ks[0] + hk * a.ks[1];
   const int64_t head = (int64_t)z * a.Hkv + hk;
+  for (int i = tid; i < (t1 - t0) * kTileRows; i += kThreads) range_s[i] = 0.f;
 
-  x8 k[4][D / 32];
-  float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  const int wkey0 = key0 + wave * kCols;
+  // adds a tile's sums, whose barrier has passed, to the range's
+  auto collect = [&](int t) {
+    if (wave == (t & (kWaves - 1))) {
+      float x = 0.f;
 #pragma unroll
-  for (int cb = 0; cb < 4; ++cb) {
-    const E* p = K + (int64_t)min(wkey0 + 16 * cb + mm, len - 1) * a.ks[2];
-#pragma unroll
-    for (int kk = 0; kk < D / 32; ++kk) k[cb][kk] = *reinterpret_cast<const x8*>(p + 32 * kk + 8 * g);
-  }
-  // rows that see the first of the keys, and of these the part's share
-  const int first_t = a.causal ? max(key0 - (len - a.T), 0) : 0;
-  const int r_first = min((int64_t)first_t * a.B * a.G, (int64_t)R) & ~(kTileRows - 1);
-  const int tiles = (R - r_first + kTileRows - 1) / kTileRows;
-  const int from = (int)((int64_t)tiles * part / a.row_parts), to = (int)((int64_t)tiles * (part + 1) / a.row_parts);
-
-  Staged<D> st;
-  float my_ref = 0.f, my_inv = 0.f;
-  int my_lim = 0;
-  auto load = [&](int t) {
-    const int r0 = r_first + t * kTileRows;
-#pragma unroll
-    for (int i = 0; i < st.kPasses; ++i) {
-      RowOf row;
-      row.set(a, min(r0 + st.kPerPass * i + tid / st.kLanes, R - 1));
-      const E* p = Q + row.b * a.qs[1] + (hk * a.G + row.g) * a.qs[2] + row.t * a.qs[3];
-      st.x[i] = *reinterpret_cast<const u32x4*>(p + 8 * (tid % st.kLanes));
-    }
-    if (tid < kTileRows) {
-      const int r = r0 + tid;
-      my_lim = 0; my_ref = INFINITY; my_inv = 0.f;
-      if (r < R) {
-        RowOf row;
-        row.set(a, r);
-        my_lim = a.causal ? min(max(len - a.T + row.t + 1, 0), len) : len;
-        if (kGiven) {
-          const float x = a.lse[(((int64_t)z * a.B + row.b) * a.H + hk * a.G + row.g) * a.T + row.t];
-          if (isinf(x)) {                          // -inf: a row that saw nothing; +inf: exp(x - inf)
-            my_lim = 0;
-          } else {
-            my_ref = x * a.l2e_hi;
-            my_inv = exp2_(-(fmaf(x, a.l2e_hi, -my_ref) + x * a.l2e_lo));
-          }
-        } else {
-          const float2 s = a.stats[head * R + r];
-          my_ref = s.x;
-          my_inv = s.y;
-        }
-      }
+      for (int v = 0; v < kWaves; ++v) x += tile_s[t & 1][v][lane];
+      range_s[(t - t0) * kTileRows + lane] += x;
     }
   };
-  if (from < to) load(from);
-  for (int t = from; t < to; ++t) {
-    const int buf = (t - from) & 1, r0 = r_first + t * kTileRows;
-    unsigned char* tile = smem + buf * kTile;
-    st.store(tile, tid);
-    if (tid < kTileRows) {
-      ref_s[buf][tid] = my_ref;
-      inv_s[buf][tid] = my_inv;
-      lim_s[buf][tid] = my_lim;
+  const int rb0 = (int)((int64_t)a.row_blocks * part / a.row_parts), rb1 = (int)((int64_t)a.row_blocks * (part + 1) / a.row_parts);
+  for (int rb = rb0; rb < rb1; ++rb) {
+    RowOf row;
+    row.set(a, min((rb + 1) * kColsWg, R) - 1);
+    const int end = min(t1, (row_limit(a, len, row.t) + kTileRows - 1) / kTileRows);   // tiles that the block's last row sees
+    if (end <= t0) continue;
+    // this wavefront's rows: operands, and what is known of a row at its lane
+    const int r0 = rb * kColsWg + wave * kCols;
+    const bool active = r0 < R;
+    x8 q[4][D / 32];
+#pragma unroll
+    for (int cb = 0; cb < 4; ++cb) {
+      row.set(a, min(r0 + 16 * cb + mm, R - 1));
+      const E* p = Q + row.b * a.qs[1] + (hk * a.G + row.g) * a.qs[2] + row.t * a.qs[3];
+#pragma unroll
+      for (int kk = 0; kk < D / 32; ++kk) q[cb][kk] = *reinterpret_cast<const x8*>(p + 32 * kk + 8 * g);
     }
-    __syncthreads();
-    if (t + 1 < to) load(t + 1);
-    const int blocks = min(R - r0 + 15, kTileRows) >> 4;
-    // some row of the tile does not see all of the wavefront's keys, or is none
-    const bool edge = __builtin_amdgcn_ballot_w64(lim_s[buf][lane] < wkey0 + kCols) != 0;
-    for (int qb = 0; qb < blocks; ++qb) {
-      x8 q[D / 32];
-#pragma unroll
-      for (int kk = 0; kk < D / 32; ++kk) q[kk] = *reinterpret_cast<const x8*>(tile + at<D>(16 * qb + mm, 4 * kk + g));
-      const f32x4 ref = *reinterpret_cast<const f32x4*>(&ref_s[buf][16 * qb + 4 * g]);
-      const f32x4 inv = *reinterpret_cast<const f32x4*>(&inv_s[buf][16 * qb + 4 * g]);
-      f32x4 s[4];
-#pragma unroll
-      for (int cb = 0; cb < 4; ++cb) {
-        s[cb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kk = 0; kk < D / 32; ++kk) s[cb] = mfma(q[kk], k[cb][kk], s[cb]);
-      }
-      if (edge) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int lim = lim_s[buf][16 * qb + 4 * g + i];
-#pragma unroll
-          for (int cb = 0; cb < 4; ++cb) {
-            const float p = exp2_(fmaf(s[cb][i], a.c2, -ref[i]));
-            if (wkey0 + 16 * cb + mm < lim) acc[cb] = fmaf(p, inv[i], acc[cb]);
-          }
+    float my_ref = INFINITY, my_inv = 0.f;
+    int my_lim = 0;                                // (of a row that is none: no key is seen)
+    if (r0 + lane < R) {
+      row.set(a, r0 + lane);
+      my_lim = row_limit(a, len, row.t);
+      if (kGiven) {
+        const float x = a.lse[(((int64_t)z * a.B + row.b) * a.H + hk * a.G + row.g) * a.T + row.t];
+        if (isinf(x)) {                            // -inf: a row that saw nothing; +inf: exp(x - inf)
+          my_lim = 0;
+        } else {
+          my_ref = x * a.l2e_hi;
+          my_inv = exp2_(-(fmaf(x, a.l2e_hi, -my_ref) + x * a.l2e_lo));
         }
       } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int cb = 0; cb < 4; ++cb) acc[cb] = fmaf(exp2_(fmaf(s[cb][i], a.c2, -ref[i])), inv[i], acc[cb]);
+        const float2 s = a.stats[head * R + r0 + lane];
+        my_ref = s.x;
+        my_inv = s.y;
       }
     }
-  }
+    wave_fence();
+    ref_s[wave][lane] = my_ref;
+    inv_s[wave][lane] = my_inv;
+    lim_s[wave][lane] = my_lim;
+    wave_fence();
+    f32x4 ref[4], inv[4];
 #pragma unroll
-  for (int cb = 0; cb < 4; ++cb) acc[cb] = column_sum(acc[cb]);
-  const float mine = g == 0 ? acc[0] : g == 1 ? acc[1] : g == 2 ? acc[2] : acc[3];
-  const int key = wkey0 + lane;
-  if (key >= len) return;
-  if (a.row_parts > 1) a.sums[((int64_t)part * a.Z * a.Hkv + head) * a.L + key] = mine;
-  else a.out[head * a.L + key] = a.prev ? a.prev[head * a.L + key] + mine : mine;
+    for (int cb = 0; cb < 4; ++cb) {
+      ref[cb] = *reinterpret_cast<const f32x4*>(&ref_s[wave][16 * cb + 4 * g]);
+      inv[cb] = *reinterpret_cast<const f32x4*>(&inv_s[wave][16 * cb + 4 * g]);
+    }
+
+    auto scores = [&](const unsigned char* tile, int kb, f32x4 (&s)[4]) {
+      x8 k[D / 32];
+#pragma unroll
+      for (int kk = 0; kk < D / 32; ++kk) k[kk] = *reinterpret_cast<const x8*>(tile + 16 * kb * 2 * D + (at<D>(mm, g) ^ (kk << 6)));
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb) s[cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < D / 32; ++kk)
+#pragma unroll
+        for (int cb = 0; cb < 4; ++cb) s[cb] = mfma(q[cb][kk], k[kk], s[cb]);
+    };
+    // of the keys of a tile, 16 * g + mm is the lane's
+    stream_keys<E, D>(
+        K, a.ks[2], len, t0, end, b0, b1, b2, tid,
+        [&](int t, const unsigned char* tile) {
+          if (t > t0) collect(t - 1);
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          if (active) {
+            // some row does not see all of the keys, or is none
+            if (__builtin_amdgcn_ballot_w64(my_lim < (t + 1) * kTileRows) != 0) return false;
+            // exponentials of a block of 16 keys stand behind the products of the next one
+            f32x4 s[2][4];
+            scores(tile, 0, s[0]);
+#pragma unroll
+            for (int kb = 0; kb < 4; ++kb) {
+              if (kb < 3) scores(tile, kb + 1, s[(kb + 1) & 1]);
+#pragma unroll
+              for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[kb] = fmaf(exp2_(fmaf(s[kb & 1][cb][i], a.c2, -ref[cb][i])), inv[cb][i], sum[kb]);
+            }
+            order_tile<D>();
+          }
+#pragma unroll
+          for (int kb = 0; kb < 4; ++kb) sum[kb] = column_sum(sum[kb]);
+          tile_s[t & 1][wave][lane] = g == 0 ? sum[0] : g == 1 ? sum[1] : g == 2 ? sum[2] : sum[3];
+          return true;
+        },
+        [&](int t, const unsigned char* tile) {
+          float mine = 0.f;
+#pragma unroll 1
+          for (int kb = 0; kb < 4; ++kb) {
+            f32x4 s[4];
+            scores(tile, kb, s);
+            float sum = 0.f;
+#pragma unroll
+            for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float p = exp2_(fmaf(s[cb][i], a.c2, -ref[cb][i])) * inv[cb][i];
+                sum += t * kTileRows + 16 * kb + mm < lim_s[wave][16 * cb + 4 * g + i] ? p : 0.f;
+              }
+            sum = column_sum(sum);
+            mine = g == kb ? sum : mine;
+          }
+          tile_s[t & 1][wave][lane] = mine;
+        });
+    __syncthreads();
+    collect(end - 1);
+    __syncthreads();                               // (tile and sums' buffers are free again)
+  }
+  __syncthreads();
+  const int key = t0 * kTileRows;
+  for (int i = tid; i < min((t1 - t0) * kTileRows, len - key); i += kThreads) {
+    if (a.row_parts > 1) a.sums[((int64_t)part * a.Z * a.Hkv + head) * a.L + key + i] = range_s[i];
+    else a.out[head * a.L + key + i] = a.prev ? a.prev[head * a.L + key + i] + range_s[i] : range_s[i];
+  }
 }
 
 __global__ __launch_bounds__(256) void sum_join_kernel(const WeightsArgs a) {
@@ -308,24 +412,30 @@ __global__ __launch_bounds__(256) void sum_join_kernel(const WeightsArgs a) {
   for (int64_t head = blockIdx.y; head < heads; head += gridDim.y) {
     if (key >= filled(a.lens, (int)(head / a.Hkv), a.L)) continue;
     float w = 0.f;
+#pragma unroll 8
     for (int p = 0; p < a.row_parts; ++p) w += a.sums[(p * heads + head) * a.L + key];
     a.out[head * a.L + key] = a.prev ? a.prev[head * a.L + key] + w : w;
   }
 }
 
-constexpr int kWorkgroups = 768;   // that the splits aim at: three on each of 256 CUs
+constexpr int kStatsSlots = 3 * 256, kSumSlots = 2 * 256;   // workgroups that are in flight together
 
 void shape_of(WeightsArgs& a, bool given) {
   const int64_t R = (int64_t)a.B * a.T * a.G, heads = (int64_t)a.Z * a.Hkv;
-  auto parts = [](int64_t units, int64_t tiles) {
-    const int64_t want = (kWorkgroups + units - 1) / units;
-    return (int)(want < tiles ? want : tiles);
+  // `slots` workgroups, as far as every part still has four tiles
+  auto parts = [](int64_t units, int64_t slots, int64_t tiles) {
+    const int64_t want = slots / units > 1 ? slots / units : 1, most = (tiles + 3) / 4;
+    return (int)(want < most ? want : most);
   };
+  const int64_t tiles = (a.L + kTileRows - 1) / kTileRows;
   a.row_blocks = (int)((R + kColsWg - 1) / kColsWg);
-  a.key_blocks = (a.L + kColsWg - 1) / kColsWg;
-  // a part has four tiles at least
-  a.key_parts = given ? 0 : parts(heads * a.row_blocks, (a.L + 4 * kTileRows - 1) / (4 * kTileRows));
-  a.row_parts = parts(heads * a.key_blocks, (R + 4 * kTileRows - 1) / (4 * kTileRows));
+  a.key_parts = given ? 0 : parts(heads * a.row_blocks, kStatsSlots, tiles);
+  // one round of ranges where there is one row block, longer ranges where there are many
+  const int64_t ranges = parts(heads * ((a.row_blocks + 3) / 4), kSumSlots, tiles);
+  a.range_tiles = (int)((tiles + ranges - 1) / ranges < kRange ? (tiles + ranges - 1) / ranges : kRange);
+  a.ranges = (int)((tiles + a.range_tiles - 1) / a.range_tiles);
+  // several rounds where there are row blocks enough, since some are shorter than others
+  a.row_parts = parts(heads * a.ranges, 4 * kSumSlots, 4 * a.row_blocks);
 }
 
 size_t stats_bytes(const WeightsArgs& a) {
@@ -335,7 +445,7 @@ size_t stats_bytes(const WeightsArgs& a) {
 template <class E, int D>
 hipError_t launch(const WeightsArgs& a, hipStream_t stream) {
   const int64_t heads = (int64_t)a.Z * a.Hkv, rows = heads * a.B * a.T * a.G;
-  const int64_t sum_blocks = heads * a.row_parts * a.key_blocks;
+  const int64_t sum_blocks = heads * a.row_parts * a.ranges;
   if (sum_blocks > 0x7fffffff) return hipErrorInvalidValue;
   if (a.lse) {
     hipLaunchKernelGGL((sum_kernel<E, D, true>), dim3((unsigned)sum_blocks), dim3(kThreads), 0, stream, a);
@@ -344,7 +454,7 @@ hipError_t launch(const WeightsArgs& a, hipStream_t stream) {
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     hipLaunchKernelGGL((stats_kernel<E, D>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
     if (a.key_parts > 1)
-      hipLaunchKernelGGL(stats_join_kernel, dim3((unsigned)((rows + 255) / 256)), dim3(256), 0, stream, a.stats, rows, a.key_parts);
+      hipLaunchKernelGGL(stats_join_kernel, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, a.stats, rows, a.key_parts);
     hipLaunchKernelGGL((sum_kernel<E, D, false>), dim3((unsigned)sum_blocks), dim3(kThreads), 0, stream, a);
   }
   if (a.row_parts > 1)
