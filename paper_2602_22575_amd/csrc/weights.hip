@@ -23,8 +23,10 @@ namespace {
 using namespace cache;
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kTileRows = 64;
-constexpr int kCols = 64;                          // query rows of a wavefront: four blocks of 16
-constexpr int kColsWg = kCols * kWaves;
+// CB: blocks of 16 query rows of a wavefront, 4 where there are more than 128 rows, so that tiles are read as rarely as possible; with
+// fewer rows 2 or 1, so that all four wavefronts have some.
+template <int CB>
+constexpr int kRowsWg = 16 * CB * kWaves;
 constexpr int kRange = 32;                         // tiles of keys of a workgroup of sum_kernel at most
 
 struct RowOf {
@@ -42,9 +44,9 @@ __device__ __forceinline__ int row_limit(const WeightsArgs& a, int len, int t) {
 
 // The order of a tile's instructions: the products of a block of 16 keys one by one, behind each its share of the three instructions a score that the
 // block before it takes.  (Left to itself the compiler waits for one block's results and then works on them.)
-template <int D>
+template <int D, int CB>
 __device__ __forceinline__ void order_tile() {
-  constexpr int kProducts = D / 8, kVector = 48 / kProducts, kReads = D / 32;
+  constexpr int kReads = D / 32, kProducts = CB * kReads, kVector = 12 / kReads;
   __builtin_amdgcn_sched_group_barrier(0x100, 2 * kReads, 0);      // LDS reads
   __builtin_amdgcn_sched_group_barrier(0x8, kProducts, 0);         // MFMA
 #pragma unroll
@@ -53,9 +55,9 @@ __device__ __forceinline__ void order_tile() {
     for (int j = 0; j < kProducts; ++j) {
       __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x402, kVector, 0);     // VALU, transcendental
-      if (kb < 2 && j % 4 == 3) __builtin_amdgcn_sched_group_barrier(0x100, kReads / (kProducts / 4), 0);
+      if (kb < 2 && j % CB == CB - 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
-  __builtin_amdgcn_sched_group_barrier(0x402, 48, 0);
+  __builtin_amdgcn_sched_group_barrier(0x402, 12 * CB, 0);
 }
 
 // Streams tiles from .. to - 1 of 64 keys through four LDS buffers, three tiles ahead of the one that is worked on: two workgroups a CU
@@ -106,53 +108,53 @@ __device__ __forceinline__ void stream_keys(const E* K, int64_t stride, int len,
 // which a sum has outgrown that look for the maximum; the others are products, exponentials and additions.
 constexpr float kRoomAbove = 0x1p90f;
 
-template <class E, int D>
+template <class E, int D, int CB>
 struct Stats {
   typedef typename Vec<E>::x8 x8;
-  x8 q[4][D / 32];
-  int lim[4];
-  float m[4], l[4];              // reference (base 2), the lane's part of the sum
+  x8 q[CB][D / 32];
+  int lim[CB];
+  float m[CB], l[CB];              // reference (base 2), the lane's part of the sum
 
-  __device__ __forceinline__ void scores(const unsigned char* tile, int kb, f32x4 (&s)[4], int mm, int g) const {
+  __device__ __forceinline__ void scores(const unsigned char* tile, int kb, f32x4 (&s)[CB], int mm, int g) const {
     x8 k[D / 32];
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk) k[kk] = *reinterpret_cast<const x8*>(tile + 16 * kb * 2 * D + (at<D>(mm, g) ^ (kk << 6)));
 #pragma unroll
-    for (int cb = 0; cb < 4; ++cb) s[cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int cb = 0; cb < CB; ++cb) s[cb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk)
 #pragma unroll
-      for (int cb = 0; cb < 4; ++cb) s[cb] = mfma(k[kk], q[cb][kk], s[cb]);
+      for (int cb = 0; cb < CB; ++cb) s[cb] = mfma(k[kk], q[cb][kk], s[cb]);
   }
   // All 64 keys seen, against the references as they are.  Exponentials of a block of 16 keys stand behind the products of the next one.
   __device__ __forceinline__ bool tile_fast(const unsigned char* tile, float c2, int mm, int g) {
-    f32x4 s[2][4];
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    f32x4 s[2][CB];
+    float sum[CB] = {};
     scores(tile, 0, s[0], mm, g);
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) {
       if (kb < 3) scores(tile, kb + 1, s[(kb + 1) & 1], mm, g);
 #pragma unroll
-      for (int cb = 0; cb < 4; ++cb)
+      for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[cb] += exp2_(fmaf(s[kb & 1][cb][i], c2, -m[cb]));
     }
-    order_tile<D>();
+    order_tile<D, CB>();
     bool fits = true;
 #pragma unroll
-    for (int cb = 0; cb < 4; ++cb) fits &= l[cb] + sum[cb] <= kRoomAbove;    // (false for NaN)
+    for (int cb = 0; cb < CB; ++cb) fits &= l[cb] + sum[cb] <= kRoomAbove;    // (false for NaN)
     if (__builtin_amdgcn_ballot_w64(!fits) != 0) return false;
 #pragma unroll
-    for (int cb = 0; cb < 4; ++cb) l[cb] += sum[cb];
+    for (int cb = 0; cb < CB; ++cb) l[cb] += sum[cb];
     return true;
   }
   __device__ __forceinline__ void tile_any(const unsigned char* tile, int key0, float c2, int mm, int g) {
 #pragma unroll 1
     for (int kb = 0; kb < 4; ++kb) {
-      f32x4 s[4];
+      f32x4 s[CB];
       scores(tile, kb, s, mm, g);
 #pragma unroll
-      for (int cb = 0; cb < 4; ++cb) {
+      for (int cb = 0; cb < CB; ++cb) {
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -170,7 +172,7 @@ struct Stats {
   }
 };
 
-template <class E, int D>
+template <class E, int D, int CB>
 __global__ __launch_bounds__(kThreads, 3) void stats_kernel(const WeightsArgs a) {
   constexpr int kTile = kTileRows * D * 2;
   __shared__ __attribute__((aligned(256))) unsigned char b0[kTile], b1[kTile], b2[kTile];
@@ -187,11 +189,11 @@ __global__ __launch_bounds__(kThreads, 3) void stats_kernel(const WeightsArgs a)
   const E* Q = static_cast<const E*>(a.Q) + z * a.qs[0];
   const E* K = static_cast<const E*>(a.K) + z * a.ks[0] + hk * a.ks[1];
 
-  Stats<E, D> w;
+  Stats<E, D, CB> w;
 #pragma unroll
-  for (int cb = 0; cb < 4; ++cb) {
+  for (int cb = 0; cb < CB; ++cb) {
     RowOf row;
-    row.set(a, min(rb * kColsWg + wave * kCols + 16 * cb + mm, R - 1));
+    row.set(a, min(rb * kRowsWg<CB> + wave * 16 * CB + 16 * cb + mm, R - 1));
     const E* p = Q + row.b * a.qs[1] + (hk * a.G + row.g) * a.qs[2] + row.t * a.qs[3];
 #pragma unroll
     for (int kk = 0; kk < D / 32; ++kk) w.q[cb][kk] = *reinterpret_cast<const typename Vec<E>::x8*>(p + 32 * kk + 8 * g);
@@ -201,12 +203,12 @@ __global__ __launch_bounds__(kThreads, 3) void stats_kernel(const WeightsArgs a)
   }
   // keys that the workgroup's first and last row see
   RowOf row;
-  row.set(a, rb * kColsWg);
+  row.set(a, rb * kRowsWg<CB>);
   const int full = row_limit(a, len, row.t) / kTileRows;
-  row.set(a, min((rb + 1) * kColsWg, R) - 1);
+  row.set(a, min((rb + 1) * kRowsWg<CB>, R) - 1);
   const int tiles = (row_limit(a, len, row.t) + kTileRows - 1) / kTileRows;
   const int from = (int)((int64_t)tiles * part / a.key_parts), to = (int)((int64_t)tiles * (part + 1) / a.key_parts);
-  const bool active = rb * kColsWg + wave * kCols < R;     // the wavefront has rows at all
+  const bool active = rb * kRowsWg<CB> + wave * 16 * CB < R;     // the wavefront has rows at all
 
   stream_keys<E, D>(K, a.ks[2], len, from, to, b0, b1, b2, tid,
                     [&](int t, const unsigned char* tile) { return !active || (t > from && t < full && w.tile_fast(tile, a.c2, mm, g)); },
@@ -214,10 +216,10 @@ __global__ __launch_bounds__(kThreads, 3) void stats_kernel(const WeightsArgs a)
   // join the four lanes of a column
   const int64_t rows = (int64_t)a.Z * a.Hkv * R;
 #pragma unroll
-  for (int cb = 0; cb < 4; ++cb) {
+  for (int cb = 0; cb < CB; ++cb) {
     const float top = column_max(w.m[cb]), ref = top == -INFINITY ? 0.f : top;
     const float sum = column_sum(w.l[cb] * exp2_(w.m[cb] - ref));
-    const int r = rb * kColsWg + wave * kCols + 16 * cb + mm;
+    const int r = rb * kRowsWg<CB> + wave * 16 * CB + 16 * cb + mm;
     if (g == 0 && r < R) {
       const int64_t i = ((int64_t)z * a.Hkv + hk) * R + r;
       // (nothing seen: a reference and factor that make every weight zero)
@@ -255,14 +257,14 @@ __global__ __launch_bounds__(256) void stats_join_kernel(float2* stats, int64_t 
 // A workgroup has a range of up to kRange tiles of keys and some of the row blocks.  Per row block its wavefronts hold 64 rows each, this time as the
 // A side, so that a lane of an accumulator block is a key and its registers are rows: a key's terms are added up inside the lane.  A tile's sums of the four
 // wavefronts meet in LDS and add to the range's.
-template <class E, int D, bool kGiven>
+template <class E, int D, int CB, bool kGiven>
 __global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs a) {
   typedef typename Vec<E>::x8 x8;
   constexpr int kTile = kTileRows * D * 2;
   __shared__ __attribute__((aligned(256))) unsigned char b0[kTile], b1[kTile], b2[kTile];
   __shared__ float range_s[kRange * kTileRows], tile_s[2][kWaves][kTileRows];
-  __shared__ __attribute__((aligned(16))) float ref_s[kWaves][kCols], inv_s[kWaves][kCols];
-  __shared__ __attribute__((aligned(16))) int lim_s[kWaves][kCols];
+  __shared__ __attribute__((aligned(16))) float ref_s[kWaves][16 * CB], inv_s[kWaves][16 * CB];
+  __shared__ __attribute__((aligned(16))) int lim_s[kWaves][16 * CB];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int mm = lane & 15, g = lane >> 4;
   // the ranges and the row blocks with the most work first: the first keys, the last rows
@@ -292,15 +294,15 @@ __global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs a) {
   const int rb0 = (int)((int64_t)a.row_blocks * part / a.row_parts), rb1 = (int)((int64_t)a.row_blocks * (part + 1) / a.row_parts);
   for (int rb = rb0; rb < rb1; ++rb) {
     RowOf row;
-    row.set(a, min((rb + 1) * kColsWg, R) - 1);
+    row.set(a, min((rb + 1) * kRowsWg<CB>, R) - 1);
     const int end = min(t1, (row_limit(a, len, row.t) + kTileRows - 1) / kTileRows);   // tiles that the block's last row sees
     if (end <= t0) continue;
     // this wavefront's rows: operands, and what is known of a row at its lane
-    const int r0 = rb * kColsWg + wave * kCols;
+    const int r0 = rb * kRowsWg<CB> + wave * 16 * CB;
     const bool active = r0 < R;
-    x8 q[4][D / 32];
+    x8 q[CB][D / 32];
 #pragma unroll
-    for (int cb = 0; cb < 4; ++cb) {
+    for (int cb = 0; cb < CB; ++cb) {
       row.set(a, min(r0 + 16 * cb + mm, R - 1));
       const E* p = Q + row.b * a.qs[1] + (hk * a.G + row.g) * a.qs[2] + row.t * a.qs[3];
 #pragma unroll
@@ -308,7 +310,7 @@ __global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs a) {
     }
     float my_ref = INFINITY, my_inv = 0.f;
     int my_lim = 0;                                // (of a row that is none: no key is seen)
-    if (r0 + lane < R) {
+    if (lane < 16 * CB && r0 + lane < R) {
       row.set(a, r0 + lane);
       my_lim = row_limit(a, len, row.t);
       if (kGiven) {
@@ -326,27 +328,29 @@ __global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs a) {
       }
     }
     wave_fence();
-    ref_s[wave][lane] = my_ref;
-    inv_s[wave][lane] = my_inv;
-    lim_s[wave][lane] = my_lim;
+    if (lane < 16 * CB) {
+      ref_s[wave][lane] = my_ref;
+      inv_s[wave][lane] = my_inv;
+      lim_s[wave][lane] = my_lim;
+    }
     wave_fence();
-    f32x4 ref[4], inv[4];
+    f32x4 ref[CB], inv[CB];
 #pragma unroll
-    for (int cb = 0; cb < 4; ++cb) {
+    for (int cb = 0; cb < CB; ++cb) {
       ref[cb] = *reinterpret_cast<const f32x4*>(&ref_s[wave][16 * cb + 4 * g]);
       inv[cb] = *reinterpret_cast<const f32x4*>(&inv_s[wave][16 * cb + 4 * g]);
     }
 
-    auto scores = [&](const unsigned char* tile, int kb, f32x4 (&s)[4]) {
+    auto scores = [&](const unsigned char* tile, int kb, f32x4 (&s)[CB]) {
       x8 k[D / 32];
 #pragma unroll
       for (int kk = 0; kk < D / 32; ++kk) k[kk] = *reinterpret_cast<const x8*>(tile + 16 * kb * 2 * D + (at<D>(mm, g) ^ (kk << 6)));
 #pragma unroll
-      for (int cb = 0; cb < 4; ++cb) s[cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int cb = 0; cb < CB; ++cb) s[cb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kk = 0; kk < D / 32; ++kk)
 #pragma unroll
-        for (int cb = 0; cb < 4; ++cb) s[cb] = mfma(q[cb][kk], k[kk], s[cb]);
+        for (int cb = 0; cb < CB; ++cb) s[cb] = mfma(q[cb][kk], k[kk], s[cb]);
     };
     // of the keys of a tile, 16 * g + mm is the lane's
     stream_keys<E, D>(
@@ -356,19 +360,19 @@ __global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs a) {
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
           if (active) {
             // some row does not see all of the keys, or is none
-            if (__builtin_amdgcn_ballot_w64(my_lim < (t + 1) * kTileRows) != 0) return false;
+            if (__builtin_amdgcn_ballot_w64(lane < 16 * CB && my_lim < (t + 1) * kTileRows) != 0) return false;
             // exponentials of a block of 16 keys stand behind the products of the next one
-            f32x4 s[2][4];
+            f32x4 s[2][CB];
             scores(tile, 0, s[0]);
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) {
               if (kb < 3) scores(tile, kb + 1, s[(kb + 1) & 1]);
 #pragma unroll
-              for (int cb = 0; cb < 4; ++cb)
+              for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[kb] = fmaf(exp2_(fmaf(s[kb & 1][cb][i], a.c2, -ref[cb][i])), inv[cb][i], sum[kb]);
             }
-            order_tile<D>();
+            order_tile<D, CB>();
           }
 #pragma unroll
           for (int kb = 0; kb < 4; ++kb) sum[kb] = column_sum(sum[kb]);
@@ -379,11 +383,11 @@ __global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs a) {
           float mine = 0.f;
 #pragma unroll 1
           for (int kb = 0; kb < 4; ++kb) {
-            f32x4 s[4];
+            f32x4 s[CB];
             scores(tile, kb, s);
             float sum = 0.f;
 #pragma unroll
-            for (int cb = 0; cb < 4; ++cb)
+            for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const float p = exp2_(fmaf(s[cb][i], a.c2, -ref[cb][i])) * inv[cb][i];
@@ -420,6 +424,11 @@ __global__ __launch_bounds__(256) void sum_join_kernel(const WeightsArgs a) {
 
 constexpr int kStatsSlots = 3 * 256, kSumSlots = 2 * 256;   // workgroups that are in flight together
 
+int row_blocks_wave(const WeightsArgs& a) {
+  const int64_t R = (int64_t)a.B * a.T * a.G;
+  return R <= 64 ? 1 : R <= 128 ? 2 : 4;
+}
+
 void shape_of(WeightsArgs& a, bool given) {
   const int64_t R = (int64_t)a.B * a.T * a.G, heads = (int64_t)a.Z * a.Hkv;
   // `slots` workgroups, as far as every part still has four tiles
@@ -428,7 +437,8 @@ void shape_of(WeightsArgs& a, bool given) {
     return (int)(want < most ? want : most);
   };
   const int64_t tiles = (a.L + kTileRows - 1) / kTileRows;
-  a.row_blocks = (int)((R + kColsWg - 1) / kColsWg);
+  const int rows_wg = 64 * row_blocks_wave(a);
+  a.row_blocks = (int)((R + rows_wg - 1) / rows_wg);
   a.key_parts = given ? 0 : parts(heads * a.row_blocks, kStatsSlots, tiles);
   // one round of ranges where there is one row block, longer ranges where there are many
   const int64_t ranges = parts(heads * ((a.row_blocks + 3) / 4), kSumSlots, tiles);
@@ -442,24 +452,30 @@ size_t stats_bytes(const WeightsArgs& a) {
   return ((size_t)a.key_parts * a.Z * a.Hkv * a.B * a.T * a.G * 8 + 255) / 256 * 256;
 }
 
-template <class E, int D>
+template <class E, int D, int CB>
 hipError_t launch(const WeightsArgs& a, hipStream_t stream) {
   const int64_t heads = (int64_t)a.Z * a.Hkv, rows = heads * a.B * a.T * a.G;
   const int64_t sum_blocks = heads * a.row_parts * a.ranges;
   if (sum_blocks > 0x7fffffff) return hipErrorInvalidValue;
   if (a.lse) {
-    hipLaunchKernelGGL((sum_kernel<E, D, true>), dim3((unsigned)sum_blocks), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((sum_kernel<E, D, CB, true>), dim3((unsigned)sum_blocks), dim3(kThreads), 0, stream, a);
   } else {
     const int64_t blocks = heads * a.row_blocks * a.key_parts;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((stats_kernel<E, D>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((stats_kernel<E, D, CB>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
     if (a.key_parts > 1)
       hipLaunchKernelGGL(stats_join_kernel, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, a.stats, rows, a.key_parts);
-    hipLaunchKernelGGL((sum_kernel<E, D, false>), dim3((unsigned)sum_blocks), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((sum_kernel<E, D, CB, false>), dim3((unsigned)sum_blocks), dim3(kThreads), 0, stream, a);
   }
   if (a.row_parts > 1)
     hipLaunchKernelGGL(sum_join_kernel, dim3((unsigned)((a.L + 255) / 256), (unsigned)(heads < 65535 ? heads : 65535)), dim3(256), 0, stream, a);
   return hipGetLastError();
+}
+
+template <class E, int D>
+hipError_t launch_rows(const WeightsArgs& a, hipStream_t stream) {
+  const int cb = row_blocks_wave(a);
+  return cb == 1 ? launch<E, D, 1>(a, stream) : cb == 2 ? launch<E, D, 2>(a, stream) : launch<E, D, 4>(a, stream);
 }
 
 }  // namespace
@@ -474,8 +490,8 @@ hipError_t launch_weights(WeightsArgs a, void* scratch, hipStream_t stream) {
   shape_of(a, a.lse != nullptr);
   a.stats = static_cast<float2*>(scratch);
   a.sums = reinterpret_cast<float*>(static_cast<char*>(scratch) + (a.lse ? 0 : stats_bytes(a)));
-  if (a.f16) return a.D == 128 ? launch<_Float16, 128>(a, stream) : launch<_Float16, 64>(a, stream);
-  return a.D == 128 ? launch<__bf16, 128>(a, stream) : launch<__bf16, 64>(a, stream);
+  if (a.f16) return a.D == 128 ? launch_rows<_Float16, 128>(a, stream) : launch_rows<_Float16, 64>(a, stream);
+  return a.D == 128 ? launch_rows<__bf16, 128>(a, stream) : launch_rows<__bf16, 64>(a, stream);
 }
 
 }  // namespace s2o
