@@ -29,6 +29,7 @@ namespace {
 using namespace cache;
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kSplitWaves = 8;                  // of a workgroup without wide blocks, where the keys are split
 constexpr int kKeys = 32, kWideKeys = 64;       // tiles of the two walks
 constexpr int kNarrowRows = 16, kWideRows = 32 * kWaves;   // query rows of a workgroup
 constexpr float kLazy = 8.0f;    // the softmax reference follows the maximum in steps of 2^8 at least (attn_tile.h)
@@ -218,23 +219,49 @@ struct Walk {
     for (; t < end; t += step) tile(t, std::true_type{});
   }
 
+  // Numerators of 32 * ST keys against the references as they are, all keys seen: no maximum is looked for.  sum: the lane's.
+  template <int ST>
+  __device__ __forceinline__ void numerators(const f32x4 (&s)[2 * ST][CB], x8 (&pb)[ST][CB], float (&sum)[CB], float c2) const {
+#pragma unroll
+    for (int st = 0; st < ST; ++st)
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        float p[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          p[j] = exp2_(fmaf(s[2 * st + (j >> 2)][cb][j & 3], c2, -m[cb]));
+          sum[cb] += p[j];
+        }
+        pb[st][cb] = __builtin_bit_cast(x8, u32x4{pack2<E>(p[0], p[1]), pack2<E>(p[2], p[3]), pack2<E>(p[4], p[5]), pack2<E>(p[6], p[7])});
+      }
+  }
+
   // Tiles from .. to - 1 of 64 keys, by all four wavefronts together.  ka, kb_, va, vb: K and V tile of even and odd steps (separate
   // arrays, so that the compiler sees that reads of one need not wait for the loads that fill another).
-  __device__ __forceinline__ void wide(const E* K, const E* V, int64_t kstride, int64_t vstride, int len, const int (&lim)[CB], int lim_all,
-                                       int from, int to, float c2, unsigned char* ka, unsigned char* kb_, unsigned char* va, unsigned char* vb, int wave, int lane) {
+  //
+  // The first tile finds the references, the last ones may have hidden keys.  For those between, if `fast`, a tile's products and exponentials
+  // are one straight run of instructions, its second half's exponentials behind its first half's products: numerators are formed
+  // against the references as they are, and a reference moves afterwards, where a tile's sum has outgrown 2^10.  Returns false where a numerator
+  // may have outgrown the element type on the way: all of it is to be done again, not fast.
+  __device__ __forceinline__ bool wide(const E* K, const E* V, int64_t kstride, int64_t vstride, int len, const int (&lim)[CB], int lim_all,
+                                       int from, int to, float c2, unsigned char* ka, unsigned char* kb_, unsigned char* va, unsigned char* vb,
+                                       int wave, int lane, bool fast) {
     constexpr int kRowLanes = D / 8, kRowsPerLoad = 64 / kRowLanes, kLoads = 16 / kRowsPerLoad;   // a wavefront loads 16 rows of each
+    constexpr float kMove = 0x1p10f, kMost = __is_same(E, __bf16) ? 0x1p60f : 0x1p15f;
     const int mm = lane & 15, g = lane >> 4, lr = lane / kRowLanes;
     // LDS takes a load's lanes in order: each fetches the chunk that belongs at its slot
     const uint32_t chunk = 16 * ((lane % kRowLanes) ^ swz<D>(lr));
     const uint32_t krow = (uint32_t)(kstride * 2), vrow = (uint32_t)(vstride * 2), koff = (uint32_t)lr * krow, voff = (uint32_t)lr * vrow;
     auto fetch = [&](int t, unsigned char* kt, unsigned char* vt) {
       const auto kg = rows_buffer(K, kstride * 2, t * kWideKeys, len, kWideKeys, 2 * D), vg = rows_buffer(V, vstride * 2, t * kWideKeys, len, kWideKeys, 2 * D);
+      uint32_t ko = koff, vo = voff, ch = chunk;
+      asm volatile("" : "+v"(ko), "+v"(vo), "+v"(ch));     // the loads' offsets are formed here, not kept in registers
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int r = 16 * wave + kRowsPerLoad * i;
-        const uint32_t c = chunk ^ (swz<D>(kRowsPerLoad * i) << 4);
-        buffer_load_to_lds(kg, koff + r * krow + c, kt + r * 2 * D);
-        buffer_load_to_lds(vg, voff + r * vrow + c, vt + r * 2 * D);
+        const uint32_t c = ch ^ (swz<D>(kRowsPerLoad * i) << 4);
+        buffer_load_to_lds(kg, ko + r * krow + c, kt + r * 2 * D);
+        buffer_load_to_lds(vg, vo + r * vrow + c, vt + r * 2 * D);
       }
     };
     // what this wavefront fetched has landed and what it read is in its registers; then everybody's
@@ -243,42 +270,99 @@ struct Walk {
       __builtin_amdgcn_s_waitcnt(0x0070);                  // vmcnt(0) lgkmcnt(0)
       asm volatile("s_barrier" ::: "memory");
     };
-    auto step = [&](int t, unsigned char* kt, unsigned char* vt, unsigned char* knext, unsigned char* vnext, auto hidden_) {
-      constexpr bool kHidden = decltype(hidden_)::value;
-      if (t + 1 < to) fetch(t + 1, knext, vnext);
-      const int key0 = t * kWideKeys;
-      f32x4 s[4][CB];
+    auto scores = [&](const unsigned char* kt, f32x4 (&s)[4][CB]) {
 #pragma unroll
       for (int kb = 0; kb < 4; ++kb) {
         x8 k[D / 32];
 #pragma unroll
         for (int kk = 0; kk < D / 32; ++kk) k[kk] = *reinterpret_cast<const x8*>(kt + 16 * kb * 2 * D + (at<D>(mm, g) ^ (kk << 6)));
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-          s[kb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int cb = 0; cb < CB; ++cb) s[kb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int kk = 0; kk < D / 32; ++kk) s[kb][cb] = mfma(k[kk], q[cb][kk], s[kb][cb]);
-        }
+        for (int kk = 0; kk < D / 32; ++kk)
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) s[kb][cb] = mfma(k[kk], q[cb][kk], s[kb][cb]);
       }
+    };
+    auto any_tile = [&](int t, unsigned char* kt, unsigned char* vt, unsigned char* knext, unsigned char* vnext) {
+      if (t + 1 < to) fetch(t + 1, knext, vnext);
+      const int key0 = t * kWideKeys;
+      f32x4 s[4][CB];
+      scores(kt, s);
       x8 pb[2][CB];
-      softmax<4, kHidden>(s, pb, key0, lim, c2, g);
-      if constexpr (kHidden) values_hidden<2>(vt, pb, key0, lim, mm, g);
-      else values<2>(vt, pb, mm, g);
+      softmax<4, true>(s, pb, key0, lim, c2, g);
+      values_hidden<2>(vt, pb, key0, lim, mm, g);
       meet();
     };
-    if (from >= to) return;
+    bool fits = true;
+    auto fast_tile = [&](int t, unsigned char* kt, unsigned char* vt, unsigned char* knext, unsigned char* vnext) {
+      if (t + 1 < to) fetch(t + 1, knext, vnext);
+      f32x4 s[4][CB];
+      scores(kt, s);
+      x8 pb[2][CB];
+      float sum[CB] = {};
+      numerators<2>(s, pb, sum, c2);
+      values<2>(vt, pb, mm, g);
+      // the order of all this
+      constexpr int kReads = D / 32, kQk = CB * kReads, kPv = CB * D / 16, kVector = 28 * CB;   // of 16 keys; of 32 keys
+      __builtin_amdgcn_sched_group_barrier(0x100, 2 * kReads, 0);
+#pragma unroll
+      for (int j = 0; j < 2 * kQk; ++j) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        if (j % CB == CB - 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < 2 * kQk; ++j) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, kVector / (2 * kQk), 0);
+        if (j >= 2 * kQk - 8) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int j = 0; j < kPv; ++j) {
+          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+          if (st == 0) __builtin_amdgcn_sched_group_barrier(0x402, kVector / kPv, 0);
+          if (j % CB == CB - 1 && j + st * kPv < 2 * kPv - 4 * CB) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+      bool moves = false;
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        l[cb] += sum[cb];
+        moves |= !(sum[cb] <= kMove);
+      }
+      if (__builtin_amdgcn_ballot_w64(moves) != 0) {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          const float most = column_max(sum[cb]);
+          fits &= !(__builtin_amdgcn_ballot_w64(!(sum[cb] <= kMost)) != 0);
+          const int up = most > kMove && most <= kMost ? __builtin_amdgcn_frexp_expf(most) : 0;
+          const float alpha = __builtin_amdgcn_ldexpf(1.0f, -up);
+          m[cb] += (float)up;
+          l[cb] *= alpha;
+#pragma unroll
+          for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[cb][db][i] *= alpha;
+        }
+      }
+      meet();
+    };
+    if (from >= to) return true;
     fetch(from, ka, va);
     meet();
-    const int full = min(to, max(from, lim_all / kWideKeys));
-    int t = from;
+    any_tile(from, ka, va, kb_, vb);
+    const int full = fast ? min(to, max(from + 1, lim_all / kWideKeys)) : from + 1;
+    int t = from + 1;
     for (; t < full; t += 2) {
-      step(t, ka, va, kb_, vb, std::false_type{});
-      if (t + 1 < full) step(t + 1, kb_, vb, ka, va, std::false_type{});
+      fast_tile(t, kb_, vb, ka, va);
+      if (t + 1 < full) fast_tile(t + 1, ka, va, kb_, vb);
     }
     for (t = full; t < to; ++t) {
       const bool odd = (t - from) & 1;
-      step(t, odd ? kb_ : ka, odd ? vb : va, odd ? ka : kb_, odd ? va : vb, std::true_type{});
+      any_tile(t, odd ? kb_ : ka, odd ? vb : va, odd ? ka : kb_, odd ? va : vb);
     }
+    return fits;
   }
 };
 
@@ -364,7 +448,7 @@ struct Block {
 };
 
 // `area(v)`: 32 x D elements of LDS for wavefront v.
-template <class E, int D, class F>
+template <class E, int D, int NW, class F>
 __device__ __forceinline__ void narrow_block(const Block<E, D>& k, F area, float2 (*ml)[16], int tid) {
   const DecodeArgs& a = k.a;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), mm = lane & 15, g = lane >> 4;
@@ -377,7 +461,7 @@ __device__ __forceinline__ void narrow_block(const Block<E, D>& k, F area, float
   for (int own = k.shared || a.direct ? 0 : 1; own < (k.shared ? 1 : 2); ++own) {
     const auto c = k.cache(own, kKeys);
     const int lim[1] = {k.limit(c, own, t_of[0])};
-    w.narrow(c.K, c.V, c.kst, c.vst, c.len, lim, k.limit(c, own, kNarrowRows * k.rb / a.G), c.from + wave, c.to, kWaves, a.c2, area(wave), lane);
+    w.narrow(c.K, c.V, c.kst, c.vst, c.len, lim, k.limit(c, own, kNarrowRows * k.rb / a.G), c.from + wave, c.to, NW, a.c2, area(wave), lane);
   }
   // join the wavefronts: 16 rows x D in 32 bits fill a wavefront's area; the 16-byte pieces of row r sit at piece ^ r
   __syncthreads();
@@ -387,14 +471,14 @@ __device__ __forceinline__ void narrow_block(const Block<E, D>& k, F area, float
   if (g == 0) ml[wave][mm] = float2{w.m[0], l};
   __syncthreads();
   const int i = tid >> 4, r = kNarrowRows * k.rb + i, d0 = (tid & 15) * (D / 16);
-  if (r >= k.rows.count) return;
+  if (i >= kNarrowRows || r >= k.rows.count) return;
   float top = -INFINITY, sum = 0.f, acc[D / 16];
 #pragma unroll
-  for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ml[v][i].x);
+  for (int v = 0; v < NW; ++v) top = fmaxf(top, ml[v][i].x);
 #pragma unroll
   for (int d = 0; d < D / 16; ++d) acc[d] = 0.f;
 #pragma unroll
-  for (int v = 0; v < kWaves; ++v) {
+  for (int v = 0; v < NW; ++v) {
     const float f = part_weight(ml[v][i].x, top);
     sum = fmaf(f, ml[v][i].y, sum);
 #pragma unroll
@@ -413,14 +497,19 @@ __device__ __forceinline__ void wide_block(const Block<E, D>& k, unsigned char* 
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), mm = lane & 15, g = lane >> 4;
   const int r0 = kWideRows * k.rb + 32 * wave;
   Walk<E, D, 2> w;
-  w.start();
   int t_of[2];
   k.load(w, r0, t_of, lane);
 #pragma unroll 1
-  for (int own = k.shared || a.direct ? 0 : 1; own < (k.shared ? 1 : 2); ++own) {
-    const auto c = k.cache(own, kWideKeys);
-    const int lim[2] = {k.limit(c, own, t_of[0]), k.limit(c, own, t_of[1])};
-    w.wide(c.K, c.V, c.kst, c.vst, c.len, lim, k.limit(c, own, kWideRows * k.rb / a.G), c.from, c.to, a.c2, ka, kb, va, vb, wave, lane);
+  for (int fast = 1; fast >= 0; --fast) {
+    w.start();
+    bool fits = true;
+#pragma unroll 1
+    for (int own = k.shared || a.direct ? 0 : 1; own < (k.shared ? 1 : 2); ++own) {
+      const auto c = k.cache(own, kWideKeys);
+      const int lim[2] = {k.limit(c, own, t_of[0]), k.limit(c, own, t_of[1])};
+      fits &= w.wide(c.K, c.V, c.kst, c.vst, c.len, lim, k.limit(c, own, kWideRows * k.rb / a.G), c.from, c.to, a.c2, ka, kb, va, vb, wave, lane, fast);
+    }
+    if (!__syncthreads_or(!fits)) break;
   }
   // O^T to rows: lane l's piece of row l % 16 is dims 16 * db + 4 * g .. + 3
 #pragma unroll
@@ -450,8 +539,10 @@ __device__ __forceinline__ void wide_block(const Block<E, D>& k, unsigned char* 
   }
 }
 
-template <class E, int D, bool kWideS, bool kWideO>
-__global__ __launch_bounds__(kThreads, kWideS ? 2 : 3) void decode_kernel(const DecodeArgs a) {
+// kNW: wavefronts of a workgroup (kWaves with wide blocks).
+template <class E, int D, bool kWideS, bool kWideO, int kNW>
+__global__ __launch_bounds__(64 * kNW, kWideS ? 2 : 1) void decode_kernel(const DecodeArgs a) {
+  static_assert(kNW == kWaves || !kWideS);
   const int tid = threadIdx.x;
   // block id -> shared units (cache, KV head, part) x row blocks, then own units (.., sequence, part) x row blocks.  Row blocks of a unit
   // read the same keys: they are given ids 8 apart, which land on one XCD at about the same time.
@@ -480,14 +571,14 @@ __global__ __launch_bounds__(kThreads, kWideS ? 2 : 3) void decode_kernel(const 
   k.slot = k.shared ? k.part : a.splits_s + k.part;
 
   constexpr int kTile = kKeys * D * 2, kWideTile = kWideKeys * D * 2;
-  __shared__ float2 ml[kWaves][16];
+  __shared__ float2 ml[kNW][16];
   if constexpr (!kWideS && !kWideO) {
-    __shared__ __attribute__((aligned(256))) unsigned char smem[kWaves * kTile];
-    narrow_block(k, [&](int v) { return smem + v * kTile; }, ml, tid);
+    __shared__ __attribute__((aligned(256))) unsigned char smem[kNW * kTile];
+    narrow_block<E, D, kNW>(k, [&](int v) { return smem + v * kTile; }, ml, tid);
   } else {
     __shared__ __attribute__((aligned(256))) unsigned char ka[kWideTile], kb[kWideTile], va[kWideTile], vb[kWideTile];
     if (kWideO || k.shared) wide_block(k, ka, kb, va, vb, tid);
-    else narrow_block(k, [&](int v) { return (v < 2 ? ka : kb) + (v & 1) * kTile; }, ml, tid);
+    else narrow_block<E, D, kNW>(k, [&](int v) { return (v < 2 ? ka : kb) + (v & 1) * kTile; }, ml, tid);
   }
 }
 
@@ -578,7 +669,9 @@ Shape shape_of(const DecodeArgs& a) {
   s.blocks_s = (int)((rows_s + rows_wg_s - 1) / rows_wg_s);
   s.blocks_o = (int)((rows_o + rows_wg_o - 1) / rows_wg_o);
   const int64_t units_s = heads * s.blocks_s, units_o = heads * a.B * s.blocks_o;
-  const int64_t slots = 256 * (s.wide_s ? 2 : 3);          // workgroups that are in flight together
+  // Workgroups that are in flight together: two wide ones on each CU.  One of eight wavefronts where all blocks are narrow: 128 KB on their
+  // way are enough (one sequence on 32K keys 31.4 us, two such workgroups a CU 35.1, three of four wavefronts 38.0), and every part more has to be joined.
+  const int64_t slots = 256 * (s.wide_s ? 2 : 1);
   if (s.direct && (a.L > 0 || units_o >= slots || a.Lo <= 512)) {
     s.splits_s = 0;
     s.splits_o = 1;
@@ -602,9 +695,10 @@ hipError_t launch(DecodeArgs a, const Shape& s, hipStream_t stream) {
   a.units_s = (int)units_s; a.units_o = (int)units_o; a.ids_s = (int)ids_s;
   if (s.parts() == 1) a.part_acc = nullptr;                // nothing to join
   const dim3 grid((unsigned)(ids_s + ids_o)), threads(kThreads);
-  if (s.wide_o) hipLaunchKernelGGL((decode_kernel<E, D, true, true>), grid, threads, 0, stream, a);
-  else if (s.wide_s) hipLaunchKernelGGL((decode_kernel<E, D, true, false>), grid, threads, 0, stream, a);
-  else hipLaunchKernelGGL((decode_kernel<E, D, false, false>), grid, threads, 0, stream, a);
+  if (s.wide_o) hipLaunchKernelGGL((decode_kernel<E, D, true, true, kWaves>), grid, threads, 0, stream, a);
+  else if (s.wide_s) hipLaunchKernelGGL((decode_kernel<E, D, true, false, kWaves>), grid, threads, 0, stream, a);
+  else if (s.direct) hipLaunchKernelGGL((decode_kernel<E, D, false, false, kWaves>), grid, threads, 0, stream, a);
+  else hipLaunchKernelGGL((decode_kernel<E, D, false, false, kSplitWaves>), grid, dim3(64 * kSplitWaves), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.part_acc) return e;
   int lanes = 1;
