@@ -38,10 +38,11 @@ constexpr float kLazy = 8.0f;    // the softmax reference follows the maximum in
 struct Rows {
   int z, b, g, count;
   __device__ __forceinline__ void find(const DecodeArgs& a, int r, int& bb, int& h, int& t) const {
-    const int per_t = b < 0 ? a.B * a.G : a.G, rest = r % per_t;
-    t = r / per_t;
-    bb = b < 0 ? rest / a.G : b;
-    h = g * a.G + rest % a.G;
+    int rest, in_group;
+    t = (b < 0 ? a.by_BG : a.by_G).by(r, rest);
+    const int sequence = a.by_G.by(rest, in_group);
+    bb = b < 0 ? sequence : b;
+    h = g * a.G + in_group;
   }
 };
 
@@ -219,27 +220,10 @@ struct Walk {
     for (; t < end; t += step) tile(t, std::true_type{});
   }
 
-  // Numerators of 32 * ST keys against the references as they are, all keys seen: no maximum is looked for.  sum: the lane's.
-  template <int ST>
-  __device__ __forceinline__ void numerators(const f32x4 (&s)[2 * ST][CB], x8 (&pb)[ST][CB], float (&sum)[CB], float c2) const {
-#pragma unroll
-    for (int st = 0; st < ST; ++st)
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb) {
-        float p[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          p[j] = exp2_(fmaf(s[2 * st + (j >> 2)][cb][j & 3], c2, -m[cb]));
-          sum[cb] += p[j];
-        }
-        pb[st][cb] = __builtin_bit_cast(x8, u32x4{pack2<E>(p[0], p[1]), pack2<E>(p[2], p[3]), pack2<E>(p[4], p[5]), pack2<E>(p[6], p[7])});
-      }
-  }
-
   // Tiles from .. to - 1 of 64 keys, by all four wavefronts together.  ka, kb_, va, vb: K and V tile of even and odd steps (separate
   // arrays, so that the compiler sees that reads of one need not wait for the loads that fill another).
   //
-  // The first tile finds the references, the last ones may have hidden keys.  For those between, if `fast`, a tile's products and exponentials
+  // The first 16 keys find the references, the last tiles may have hidden keys.  For the others, if `fast`, a tile's products and exponentials
   // are one straight run of instructions, its second half's exponentials behind its first half's products: numerators are formed
   // against the references as they are, and a reference moves afterwards, where a tile's sum has outgrown 2^10.  Returns false where a numerator
   // may have outgrown the element type on the way: all of it is to be done again, not fast.
@@ -297,34 +281,69 @@ struct Walk {
     bool fits = true;
     auto fast_tile = [&](int t, unsigned char* kt, unsigned char* vt, unsigned char* knext, unsigned char* vnext) {
       if (t + 1 < to) fetch(t + 1, knext, vnext);
+      // K operands in pairs p = (32-key half, 32 dims), two pairs ahead of their products; V operands behind them, four ahead.  Every
+      // product, and what stands behind it, is a scheduling region of its own.
+      constexpr int kDims = D / 32, kPairs = 2 * kDims, kBlocks = D / 16, kAhead = 4;
+      constexpr int kEach = 16 / (2 * kDims * CB);         // scores a lane that are worked on behind a product: 16 a half
+      static_assert(CB == 2 && kEach * 2 * kDims * CB == 16 && kBlocks == 2 * kDims);
       f32x4 s[4][CB];
-      scores(kt, s);
-      x8 pb[2][CB];
-      float sum[CB] = {};
-      numerators<2>(s, pb, sum, c2);
-      values<2>(vt, pb, mm, g);
-      // the order of all this
-      constexpr int kReads = D / 32, kQk = CB * kReads, kPv = CB * D / 16, kVector = 28 * CB;   // of 16 keys; of 32 keys
-      __builtin_amdgcn_sched_group_barrier(0x100, 2 * kReads, 0);
+      x8 kf[kPairs][2], vf[2 * kBlocks], pb[2][CB];
+      float sum[CB] = {}, p[2][16];
+      auto read_keys = [&](int pair) {
 #pragma unroll
-      for (int j = 0; j < 2 * kQk; ++j) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        if (j % CB == CB - 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
+        for (int e = 0; e < 2; ++e)
+          kf[pair][e] = *reinterpret_cast<const x8*>(kt + 16 * (2 * (pair / kDims) + e) * 2 * D + (at<D>(mm, g) ^ ((pair % kDims) << 6)));
+      };
+      auto read_values = [&](int f) { vf[f] = __builtin_bit_cast(x8, value_operand(vt + (f / kBlocks) * 64 * D, f % kBlocks, mm, g)); };
+      auto numerators = [&](int half, int first) {         // of the half's scores first .. first + kEach - 1: 8 * column block + key
 #pragma unroll
-      for (int j = 0; j < 2 * kQk; ++j) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x402, kVector / (2 * kQk), 0);
-        if (j >= 2 * kQk - 8) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-#pragma unroll
-      for (int st = 0; st < 2; ++st)
-#pragma unroll
-        for (int j = 0; j < kPv; ++j) {
-          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-          if (st == 0) __builtin_amdgcn_sched_group_barrier(0x402, kVector / kPv, 0);
-          if (j % CB == CB - 1 && j + st * kPv < 2 * kPv - 4 * CB) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        for (int x = first; x < first + kEach; ++x) {
+          const int cb = x >> 3, j = x & 7;
+          p[half][x] = exp2_(fmaf(s[2 * half + (j >> 2)][cb][j & 3], c2, -m[cb]));
+          sum[cb] += p[half][x];
         }
+      };
+      auto pack = [&](int half) {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          u32x4 w;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w[j] = pack2<E>(p[half][8 * cb + 2 * j], p[half][8 * cb + 2 * j + 1]);
+          pb[half][cb] = __builtin_bit_cast(x8, w);
+        }
+      };
+      read_keys(0);
+      read_keys(1);
+#pragma unroll
+      for (int pair = 0; pair < kPairs; ++pair) {
+        const int half = pair / kDims, kk = pair % kDims;
+        if (pair + 2 < kPairs) read_keys(pair + 2);
+        else { read_values(2 * (pair + 2 - kPairs)); read_values(2 * (pair + 2 - kPairs) + 1); }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) {
+            f32x4& x = s[2 * half + e][cb];
+            x = mfma(kf[pair][e], q[cb][kk], kk == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : x);
+            if (half == 1) numerators(0, kEach * (4 * kk + 2 * e + cb));
+            __builtin_amdgcn_sched_barrier(0);
+          }
+      }
+      pack(0);
+#pragma unroll
+      for (int f = 0; f < 2 * kBlocks; ++f) {
+        const int half = f / kBlocks, db = f % kBlocks;
+        if (f == kBlocks) pack(1);
+        if (f + kAhead < 2 * kBlocks) read_values(f + kAhead);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          o[cb][db] = mfma(vf[f], pb[half][cb], o[cb][db]);
+          if (half == 0) numerators(1, kEach * (2 * db + cb));
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
       bool moves = false;
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
@@ -351,14 +370,25 @@ struct Walk {
     if (from >= to) return true;
     fetch(from, ka, va);
     meet();
-    any_tile(from, ka, va, kb_, vb);
-    const int full = fast ? min(to, max(from + 1, lim_all / kWideKeys)) : from + 1;
-    int t = from + 1;
-    for (; t < full; t += 2) {
-      fast_tile(t, kb_, vb, ka, va);
-      if (t + 1 < full) fast_tile(t + 1, ka, va, kb_, vb);
+    const int full = fast ? min(to, lim_all / kWideKeys) : from;
+    int t = from;
+    if (t < full) {
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < D / 32; ++kk) s = mfma(*reinterpret_cast<const x8*>(ka + (at<D>(mm, g) ^ (kk << 6))), q[cb][kk], s);
+        const float top = column_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))) * c2;
+        const float first = m[cb] == -INFINITY ? top : m[cb];   // (a second cache goes on with the first one's)
+        m[cb] = first;
+        fits &= __builtin_amdgcn_ballot_w64(!(fabsf(first) < INFINITY)) == 0;
+      }
     }
-    for (t = full; t < to; ++t) {
+    for (; t < full; t += 2) {
+      fast_tile(t, ka, va, kb_, vb);
+      if (t + 1 < full) fast_tile(t + 1, kb_, vb, ka, va);
+    }
+    for (t = max(from, full); t < to; ++t) {
       const bool odd = (t - from) & 1;
       any_tile(t, odd ? kb_ : ka, odd ? vb : va, odd ? ka : kb_, odd ? va : vb);
     }
@@ -443,7 +473,11 @@ struct Block {
     c.to = (int)((int64_t)tiles * (part + 1) / splits);
     return c;
   }
-  // rows that query token t sees; what the row block's first row does, all do
+  // rows that query token t sees, and those that all of the block's rows do: its first one's
+  __device__ __forceinline__ int limit_all(const Cache& c, bool own, int rows_block) const {
+    int rest;
+    return limit(c, own, a.by_G.by(rows_block * rb, rest));
+  }
   __device__ __forceinline__ int limit(const Cache& c, bool own, int t) const { return own ? min(max(c.len - a.T + t + 1, 0), c.len) : c.len; }
 };
 
@@ -461,7 +495,7 @@ __device__ __forceinline__ void narrow_block(const Block<E, D>& k, F area, float
   for (int own = k.shared || a.direct ? 0 : 1; own < (k.shared ? 1 : 2); ++own) {
     const auto c = k.cache(own, kKeys);
     const int lim[1] = {k.limit(c, own, t_of[0])};
-    w.narrow(c.K, c.V, c.kst, c.vst, c.len, lim, k.limit(c, own, kNarrowRows * k.rb / a.G), c.from + wave, c.to, NW, a.c2, area(wave), lane);
+    w.narrow(c.K, c.V, c.kst, c.vst, c.len, lim, k.limit_all(c, own, kNarrowRows), c.from + wave, c.to, NW, a.c2, area(wave), lane);
   }
   // join the wavefronts: 16 rows x D in 32 bits fill a wavefront's area; the 16-byte pieces of row r sit at piece ^ r
   __syncthreads();
@@ -507,7 +541,7 @@ __device__ __forceinline__ void wide_block(const Block<E, D>& k, unsigned char* 
     for (int own = k.shared || a.direct ? 0 : 1; own < (k.shared ? 1 : 2); ++own) {
       const auto c = k.cache(own, kWideKeys);
       const int lim[2] = {k.limit(c, own, t_of[0]), k.limit(c, own, t_of[1])};
-      fits &= w.wide(c.K, c.V, c.kst, c.vst, c.len, lim, k.limit(c, own, kWideRows * k.rb / a.G), c.from, c.to, a.c2, ka, kb, va, vb, wave, lane, fast);
+      fits &= w.wide(c.K, c.V, c.kst, c.vst, c.len, lim, k.limit_all(c, own, kWideRows), c.from, c.to, a.c2, ka, kb, va, vb, wave, lane, fast);
     }
     if (!__syncthreads_or(!fits)) break;
   }
@@ -546,29 +580,21 @@ __global__ __launch_bounds__(64 * kNW, kWideS ? 2 : 1) void decode_kernel(const 
   const int tid = threadIdx.x;
   // block id -> shared units (cache, KV head, part) x row blocks, then own units (.., sequence, part) x row blocks.  Row blocks of a unit
   // read the same keys: they are given ids 8 apart, which land on one XCD at about the same time.
-  int id = blockIdx.x;
+  int id = blockIdx.x, in_turn, part;
   Block<E, D> k{a};
   k.shared = id < a.ids_s;
-  const int blocks = k.shared ? a.blocks_s : a.blocks_o, units = k.shared ? a.units_s : a.units_o;
   if (!k.shared) id -= a.ids_s;
-  const int turn = id / (8 * blocks);
-  id -= turn * 8 * blocks;
-  k.rb = id / 8;
-  int unit = turn * 8 + id % 8;
-  if (unit >= units) return;                       // an id that only rounds the grid up
-  k.rows.g = unit % a.Hkv;
-  unit /= a.Hkv;
-  if (k.shared) {
-    k.rows.b = -1;
-    k.rows.count = a.B * a.T * a.G;
-  } else {
-    k.rows.b = unit % a.B;
-    unit /= a.B;
-    k.rows.count = a.T * a.G;
-  }
-  k.rows.z = unit % a.Z;
-  k.part = unit / a.Z;
-  k.slot = k.shared ? k.part : a.splits_s + k.part;
+  const int turn = (k.shared ? a.by_blocks_s : a.by_blocks_o).by(id, in_turn);
+  k.rb = in_turn / 8;
+  int unit = turn * 8 + in_turn % 8;
+  if (unit >= (k.shared ? a.units_s : a.units_o)) return;  // an id that only rounds the grid up
+  unit = a.by_Hkv.by(unit, k.rows.g);
+  k.rows.b = -1;
+  if (!k.shared) unit = a.by_B.by(unit, k.rows.b);
+  part = a.by_Z.by(unit, k.rows.z);
+  k.rows.count = (k.shared ? a.B : 1) * a.T * a.G;
+  k.part = part;
+  k.slot = k.shared ? part : a.splits_s + part;
 
   constexpr int kTile = kKeys * D * 2, kWideTile = kWideKeys * D * 2;
   __shared__ float2 ml[kNW][16];
@@ -596,25 +622,25 @@ __global__ __launch_bounds__(256) void decode_join_kernel(const DecodeArgs a, in
   float top = -INFINITY, sum = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   if (live) {
-    for (int p0 = pl; p0 < parts; p0 += 8 * lanes) {       // up to eight parts' loads in flight
-      float2 s[8];
-      f32x4 v[8];
+    for (int p0 = pl; p0 < parts; p0 += 4 * lanes) {       // four parts' loads in flight
+      float2 s[4];
+      f32x4 v[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < 4; ++j) {
         const int p = min(p0 + j * lanes, parts - 1);
         s[j] = a.part_ml[p * all_rows + row];
         v[j] = *reinterpret_cast<const f32x4*>(a.part_acc + (p * all_rows + row) * D + 4 * quad);
       }
       float next = top;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) next = fmaxf(next, s[j].x);
+      for (int j = 0; j < 4; ++j) next = fmaxf(next, s[j].x);
       const float f0 = part_weight(top, next);
       top = next;
       sum *= f0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[i] *= f0;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < 4; ++j) {
         if (p0 + j * lanes < parts) {
           const float f = part_weight(s[j].x, top);
           sum = fmaf(f, s[j].y, sum);
@@ -640,11 +666,8 @@ __global__ __launch_bounds__(256) void decode_join_kernel(const DecodeArgs a, in
     }
   }
   if (!live) return;
-  const int t = (int)(row % a.T);
-  int64_t i = row / a.T;
-  const int h = (int)(i % a.H);
-  i /= a.H;
-  const int b = (int)(i % a.B), z = (int)(i / a.B);
+  int t, h, b;
+  const int z = a.by_B.by(a.by_H.by(a.by_T.by((int)row, t), h), b);
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
   E* o = static_cast<E*>(a.O) + z * a.os[0] + b * a.os[1] + h * a.os[2] + t * a.os[3] + 4 * quad;
   *reinterpret_cast<u32x2*>(o) = u32x2{pack2<E>(acc[0] * inv, acc[1] * inv), pack2<E>(acc[2] * inv, acc[3] * inv)};
@@ -693,6 +716,9 @@ hipError_t launch(DecodeArgs a, const Shape& s, hipStream_t stream) {
   const int64_t ids_s = (units_s + 7) / 8 * 8 * s.blocks_s, ids_o = (units_o + 7) / 8 * 8 * s.blocks_o;
   if (ids_s + ids_o <= 0 || ids_s + ids_o > 0x7fffffff) return hipErrorInvalidValue;
   a.units_s = (int)units_s; a.units_o = (int)units_o; a.ids_s = (int)ids_s;
+  a.by_blocks_s = Divisor(8 * s.blocks_s); a.by_blocks_o = Divisor(8 * s.blocks_o);
+  a.by_Z = Divisor(a.Z); a.by_B = Divisor(a.B); a.by_H = Divisor(a.H); a.by_Hkv = Divisor(a.Hkv);
+  a.by_G = Divisor(a.G); a.by_BG = Divisor(a.B * a.G); a.by_T = Divisor(a.T);
   if (s.parts() == 1) a.part_acc = nullptr;                // nothing to join
   const dim3 grid((unsigned)(ids_s + ids_o)), threads(kThreads);
   if (s.wide_o) hipLaunchKernelGGL((decode_kernel<E, D, true, true, kWaves>), grid, threads, 0, stream, a);

@@ -96,6 +96,25 @@ hipError_t launch_prefix(const AttnArgs& a, hipStream_t stream);
 // Notes a failed HIP call for s2o_last_hip_error; S2O_EHIP.
 int hip_fail(hipError_t e);
 
+// Quotient and rest of non-negative numbers below 2^31 by d = 1 .. 2^31 - 1 that the host has prepared: a product's upper half instead of the
+// forty instructions of a division.  mul = ceil(2^(31 + s) / d), 2^(s-1) < d <= 2^s: n * mul / 2^(31 + s) is off by less than 1/d above.
+struct Divisor {
+  uint32_t mul, shift, d;
+  Divisor() = default;
+  __host__ explicit Divisor(uint32_t d_) : mul(0), shift(0), d(d_) {
+    if (d <= 1) return;
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    mul = (uint32_t)(((1ull << (31 + s)) + d - 1) / d);
+    shift = s - 1;
+  }
+  __device__ __forceinline__ int by(int n, int& rest) const {
+    const uint32_t q = mul ? __umulhi((uint32_t)n, mul) >> shift : (uint32_t)n;
+    rest = n - (int)(q * d);
+    return (int)q;
+  }
+};
+
 // s2o_decode (decode.hip).  qs, oks, ovs, os: strides for (z, b, head, row); ks, vs: (z, head, row).
 struct DecodeArgs {
   const void *Q, *K, *V, *oK, *oV;
@@ -110,6 +129,7 @@ struct DecodeArgs {
   float2* part_ml;
   int blocks_s, splits_s, blocks_o, splits_o, direct;
   int units_s, units_o, ids_s;   // (cache, KV head, part) and (.., sequence, part); block ids of shared row blocks
+  Divisor by_blocks_s, by_blocks_o, by_Z, by_B, by_H, by_Hkv, by_G, by_BG, by_T;   // (by_blocks: eight units' blocks)
 };
 size_t decode_scratch_bytes(const DecodeArgs& a);
 hipError_t launch_decode(DecodeArgs a, void* scratch, hipStream_t stream);
