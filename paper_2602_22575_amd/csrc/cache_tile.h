@@ -78,6 +78,24 @@ __device__ __forceinline__ float column_sum(float x) {
   return __uint_as_float(q.x) + __uint_as_float(q.y);
 }
 
+// Asks for every 64-byte line of the kernel's arguments at once.
+template <class A>
+__device__ __forceinline__ void touch_args() {
+  typedef const __attribute__((address_space(4))) volatile uint32_t* Words;
+  const Words p = (Words)__builtin_amdgcn_kernarg_segment_ptr();
+  uint32_t x = 0;
+#pragma unroll
+  for (size_t i = 0; i < sizeof(A) / 4; i += 16) x |= p[i];
+  asm volatile("" ::"s"(x));
+}
+
+// The lane's number, made anew where it is asked for.
+__device__ __forceinline__ int lane_id() {
+  int n = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+  asm volatile("" : "+v"(n));
+  return n;
+}
+
 // A wavefront's own LDS writes stand before its own LDS reads: the hardware keeps their order, this keeps the compiler's.
 __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -85,6 +103,16 @@ __device__ __forceinline__ void wave_fence() {
 }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The arguments of a kernel whose one parameter is an A, to be read from here on: what a stretch of code needs of them is loaded there, and does
+// not stay in scalar registers from the first stretch to the last (where they do not all fit).
+template <class A>
+__device__ __forceinline__ const A& kernel_args() {
+  typedef const __attribute__((address_space(4))) A* Pointer;
+  Pointer p = (Pointer)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const A*)p;
+}
 
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 

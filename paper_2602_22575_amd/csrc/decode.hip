@@ -118,9 +118,13 @@ struct Walk {
   }
 
   // The V^T operand of 16 dims and 32 keys whose rows start at `vt` in LDS: keys 4 * g + (0..3) and 16 + 4 * g + (0..3).
+  // kMade: the place of the upper dims is made from that of the lower ones each time, not kept in a register.
+  template <bool kMade = false>
   static __device__ __forceinline__ u32x4 value_operand(const unsigned char* vt, int db, int mm, int g) {
     typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-    const unsigned char* p = vt + ((at<D>(4 * g + (mm >> 2), (mm & 3) >> 1) + 8 * (mm & 1)) ^ (db << 5));
+    uint32_t place = (at<D>(4 * g + (mm >> 2), (mm & 3) >> 1) + 8 * (mm & 1)) ^ ((kMade ? db & 3 : db) << 5);
+    if (kMade && db >= 4) asm volatile("v_xor_b32 %0, 0x80, %1" : "=v"(place) : "v"(place));
+    const unsigned char* p = vt + place;
     const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
     const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 16 * 2 * D));
     const u32x2 w0 = __builtin_bit_cast(u32x2, v0), w1 = __builtin_bit_cast(u32x2, v1);
@@ -169,12 +173,14 @@ struct Walk {
     }
   }
 
-  // Tiles first, first + step, .. < end of a cache of `len` rows; the lane's column cb sees the first lim[cb] of them, every column the
-  // first lim_all.  vt: the wavefront's 32 x D elements of LDS.
+  // Tiles first, first + step, .. < end of a cache of `len` rows.  `rows` loads the queries, behind the first keys, and tells what they see: the
+  // lane's column cb the first lim[cb] rows, every column the first lim_all.  vt: the wavefront's 32 x D elements of LDS.
   // (The tiles that some column does not see all of, the last ones, have a loop of their own here and in `wide`: what they need
   // beside the products would cost every tile registers.)
-  __device__ __forceinline__ void narrow(const E* K, const E* V, int64_t kstride, int64_t vstride, int len, const int (&lim)[CB], int lim_all,
-                                         int first, int end, int step, float c2, unsigned char* vt, int lane) {
+  template <class F>
+  __device__ __forceinline__ void narrow(const E* K, const E* V, int64_t kstride, int64_t vstride, int len, int first, int end, int step,
+                                         float c2, unsigned char* vt, int lane, F rows) {
+    if (first >= end) return;
     constexpr int kRowLanes = D / 8, kLoads = D / 16;      // 16-byte pieces a row; V loads a lane
     constexpr int kRowsPerLoad = 64 / kRowLanes;
     const int mm = lane & 15, g = lane >> 4, lr = lane / kRowLanes;
@@ -190,6 +196,7 @@ struct Walk {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) vr[i] = buffer_load(vtile, voff + kRowsPerLoad * i * (uint32_t)(vstride * 2));
     };
+    int lim[CB], lim_all;
     auto tile = [&](int t, auto hidden_) {
       constexpr bool kHidden = decltype(hidden_)::value;
       const int key0 = t * kKeys;
@@ -214,32 +221,36 @@ struct Walk {
       if constexpr (kHidden) values_hidden<1>(vt, pb, key0, lim, mm, g);
       else values<1>(vt, pb, mm, g);
     };
-    if (first < end) load(first);
+    load(first);
+    rows(lim, lim_all);
     int t = first;
     for (; t < end && (t + 1) * kKeys <= lim_all; t += step) tile(t, std::false_type{});
     for (; t < end; t += step) tile(t, std::true_type{});
   }
 
-  // Tiles from .. to - 1 of 64 keys, by all four wavefronts together.  ka, kb_, va, vb: K and V tile of even and odd steps (separate
+  // Tiles from .. to - 1 of 64 keys, by all four wavefronts together; `rows` as above.  ka, kb_, va, vb: K and V tile of even and odd steps (separate
   // arrays, so that the compiler sees that reads of one need not wait for the loads that fill another).
   //
   // The first 16 keys find the references, the last tiles may have hidden keys.  For the others, if `fast`, a tile's products and exponentials
   // are one straight run of instructions, its second half's exponentials behind its first half's products: numerators are formed
   // against the references as they are, and a reference moves afterwards, where a tile's sum has outgrown 2^10.  Returns false where a numerator
   // may have outgrown the element type on the way: all of it is to be done again, not fast.
-  __device__ __forceinline__ bool wide(const E* K, const E* V, int64_t kstride, int64_t vstride, int len, const int (&lim)[CB], int lim_all,
-                                       int from, int to, float c2, unsigned char* ka, unsigned char* kb_, unsigned char* va, unsigned char* vb,
-                                       int wave, int lane, bool fast) {
+  template <class F>
+  __device__ __forceinline__ bool wide(const E* K, const E* V, int64_t kstride, int64_t vstride, int len, int from, int to, float c2,
+                                       unsigned char* ka, unsigned char* kb_, unsigned char* va, unsigned char* vb, int wave, int lane,
+                                       bool fast, F rows) {
+    if (from >= to) return true;
+    int lim[CB], lim_all;
     constexpr int kRowLanes = D / 8, kRowsPerLoad = 64 / kRowLanes, kLoads = 16 / kRowsPerLoad;   // a wavefront loads 16 rows of each
     constexpr float kMove = 0x1p10f, kMost = __is_same(E, __bf16) ? 0x1p60f : 0x1p15f;
-    const int mm = lane & 15, g = lane >> 4, lr = lane / kRowLanes;
-    // LDS takes a load's lanes in order: each fetches the chunk that belongs at its slot
-    const uint32_t chunk = 16 * ((lane % kRowLanes) ^ swz<D>(lr));
-    const uint32_t krow = (uint32_t)(kstride * 2), vrow = (uint32_t)(vstride * 2), koff = (uint32_t)lr * krow, voff = (uint32_t)lr * vrow;
+    const int mm = lane & 15, g = lane >> 4;
+    // LDS takes a load's lanes in order: each fetches the chunk that belongs at its slot.  (Offsets are made for every tile: kept, they would
+    // be put aside in memory.)
+    const uint32_t krow = (uint32_t)(kstride * 2), vrow = (uint32_t)(vstride * 2);
     auto fetch = [&](int t, unsigned char* kt, unsigned char* vt) {
       const auto kg = rows_buffer(K, kstride * 2, t * kWideKeys, len, kWideKeys, 2 * D), vg = rows_buffer(V, vstride * 2, t * kWideKeys, len, kWideKeys, 2 * D);
-      uint32_t ko = koff, vo = voff, ch = chunk;
-      asm volatile("" : "+v"(ko), "+v"(vo), "+v"(ch));     // the loads' offsets are formed here, not kept in registers
+      const int ln = lane_id(), lr = ln / kRowLanes;
+      const uint32_t ko = (uint32_t)lr * krow, vo = (uint32_t)lr * vrow, ch = 16 * ((ln % kRowLanes) ^ swz<D>(lr));
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int r = 16 * wave + kRowsPerLoad * i;
@@ -294,7 +305,7 @@ struct Walk {
         for (int e = 0; e < 2; ++e)
           kf[pair][e] = *reinterpret_cast<const x8*>(kt + 16 * (2 * (pair / kDims) + e) * 2 * D + (at<D>(mm, g) ^ ((pair % kDims) << 6)));
       };
-      auto read_values = [&](int f) { vf[f] = __builtin_bit_cast(x8, value_operand(vt + (f / kBlocks) * 64 * D, f % kBlocks, mm, g)); };
+      auto read_values = [&](int f) { vf[f] = __builtin_bit_cast(x8, value_operand<true>(vt + (f / kBlocks) * 64 * D, f % kBlocks, mm, g)); };
       auto numerators = [&](int half, int first) {         // of the half's scores first .. first + kEach - 1: 8 * column block + key
 #pragma unroll
         for (int x = first; x < first + kEach; ++x) {
@@ -367,8 +378,8 @@ struct Walk {
       }
       meet();
     };
-    if (from >= to) return true;
     fetch(from, ka, va);
+    rows(lim, lim_all);
     meet();
     const int full = fast ? min(to, lim_all / kWideKeys) : from;
     int t = from;
@@ -407,34 +418,44 @@ __device__ __forceinline__ float natural_lse(float top, float sum) {
 // shared ones first.
 template <class E, int D>
 struct Block {
-  const DecodeArgs& a;
   Rows rows;
-  int rb, part, slot;
+  int rb, part;
   bool shared;
 
-  // Part and result of the row that (the lane's group of) D / 16 threads hold.
-  __device__ __forceinline__ void write(int r, int d0, const float (&acc)[D / 16], float top, float sum, bool first) const {
-    int b, h, t;
-    rows.find(a, r, b, h, t);
-    const int z = rows.z;
-    const int64_t all_rows = (int64_t)a.Z * a.B * a.H * a.T, row = (((int64_t)z * a.B + b) * a.H + h) * a.T + t;
-    if (a.part_acc) {
-      float* p = a.part_acc + (slot * all_rows + row) * D + d0;
+  float* acc;                      // the part's states of the block's rows (null: nothing is joined, results are written)
+  float2* ml;
+
+  // [part][cache, KV head][row], behind them [part][cache, sequence, KV head][row].
+  __device__ __forceinline__ void find_states(const DecodeArgs& a, int rows_block) {
+    const int64_t unit = shared ? (int64_t)rows.z * a.Hkv + rows.g : ((int64_t)rows.z * a.B + rows.b) * a.Hkv + rows.g;
+    const int64_t i = (shared ? part : a.splits_s + part) * a.rows + unit * rows.count + rows_block * rb;
+    acc = a.part_acc ? a.part_acc + i * D : nullptr;
+    ml = a.part_ml + i;
+  }
+  // Part or result of the narrow block's row i, of which the thread holds D / 16 dims.
+  __device__ __forceinline__ void write(int i, int d0, const float (&x)[D / 16], float top, float sum, bool first) const {
+    if (acc) {
+      float* p = acc + i * D + d0;
 #pragma unroll
-      for (int d = 0; d < D / 16; d += 4) *reinterpret_cast<f32x4*>(p + d) = f32x4{acc[d], acc[d + 1], acc[d + 2], acc[d + 3]};
-      if (first) a.part_ml[slot * all_rows + row] = float2{top, sum};
+      for (int d = 0; d < D / 16; d += 4) *reinterpret_cast<f32x4*>(p + d) = f32x4{x[d], x[d + 1], x[d + 2], x[d + 3]};
+      if (first) ml[i] = float2{top, sum};
     } else {
+      const DecodeArgs& a = kernel_args<DecodeArgs>();
+      int b, h, t;
+      rows.find(a, kNarrowRows * rb + i, b, h, t);
+      const int z = rows.z;
       const float inv = sum == 0.f ? 0.f : 1.0f / sum;
       uint32_t* o = reinterpret_cast<uint32_t*>(static_cast<E*>(a.O) + z * a.os[0] + b * a.os[1] + h * a.os[2] + t * a.os[3] + d0);
 #pragma unroll
-      for (int d = 0; d < D / 16; d += 2) o[d / 2] = pack2<E>(acc[d] * inv, acc[d + 1] * inv);
-      if (a.lse && first) a.lse[row] = natural_lse(top, sum);
+      for (int d = 0; d < D / 16; d += 2) o[d / 2] = pack2<E>(x[d] * inv, x[d + 1] * inv);
+      if (a.lse && first) a.lse[(((int64_t)z * a.B + b) * a.H + h) * a.T + t] = natural_lse(top, sum);
     }
   }
 
   // Loads the query rows from r0 on into the columns of `w`; tokens of the rows.
   template <int CB>
   __device__ __forceinline__ void load(Walk<E, D, CB>& w, int r0, int (&t_of)[CB], int lane) const {
+    const DecodeArgs& a = kernel_args<DecodeArgs>();
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       int b, h;
@@ -445,57 +466,75 @@ struct Block {
     }
   }
 
+  __device__ __forceinline__ int first_cache() const { return shared || kernel_args<DecodeArgs>().direct ? 0 : 1; }
   // The cache that the block walks (own: its sequence's), and this part's tiles of `keys` rows.
   struct Cache {
     const E *K, *V;
     int64_t kst, vst;
     int len, from, to;
+    float c2;
   };
   __device__ __forceinline__ Cache cache(bool own, int keys) const {
+    const DecodeArgs& a = kernel_args<DecodeArgs>();
     const int z = rows.z, hk = rows.g, b = rows.b;
     Cache c;
-    int splits = 1;
+    c.c2 = a.c2;
     if (own) {
       c.K = static_cast<const E*>(a.oK) + z * a.oks[0] + b * a.oks[1] + hk * a.oks[2];
       c.V = static_cast<const E*>(a.oV) + z * a.ovs[0] + b * a.ovs[1] + hk * a.ovs[2];
       c.kst = a.oks[3]; c.vst = a.ovs[3];
       c.len = filled(a.own_lens, z * a.B + b, a.Lo);
-      if (!a.direct) splits = a.splits_o;
     } else {
       c.K = static_cast<const E*>(a.K) + z * a.ks[0] + hk * a.ks[1];
       c.V = static_cast<const E*>(a.V) + z * a.vs[0] + hk * a.vs[1];
       c.kst = a.ks[2]; c.vst = a.vs[2];
       c.len = filled(a.lens, z, a.L);
-      if (!a.direct) splits = a.splits_s;
     }
-    const int tiles = (c.len + keys - 1) / keys;
-    c.from = (int)((int64_t)tiles * part / splits);
-    c.to = (int)((int64_t)tiles * (part + 1) / splits);
+    // as many tiles a part, or one more in the first ones
+    int more, tiles = (c.len + keys - 1) / keys;
+    if (a.direct) {
+      c.from = 0;
+    } else {
+      tiles = (own ? a.by_splits_o : a.by_splits_s).by(tiles, more);
+      c.from = part * tiles + min(part, more);
+      tiles += part < more;
+    }
+    c.to = c.from + tiles;
     return c;
   }
-  // rows that query token t sees, and those that all of the block's rows do: its first one's
-  __device__ __forceinline__ int limit_all(const Cache& c, bool own, int rows_block) const {
+  // Rows that query token t_of[cb] sees, and those that all of the block's rows do: its first one's.
+  template <int CB>
+  __device__ __forceinline__ void limits(const Cache& c, bool own, int rows_block, const int (&t_of)[CB], int (&lim)[CB], int& lim_all) const {
+    lim_all = c.len;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) lim[cb] = c.len;
+    if (!own) return;
+    const DecodeArgs& a = kernel_args<DecodeArgs>();
     int rest;
-    return limit(c, own, a.by_G.by(rows_block * rb, rest));
+    const int T = a.T, t = a.by_G.by(rows_block * rb, rest);
+    lim_all = min(max(c.len - T + t + 1, 0), c.len);
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) lim[cb] = min(max(c.len - T + t_of[cb] + 1, 0), c.len);
   }
-  __device__ __forceinline__ int limit(const Cache& c, bool own, int t) const { return own ? min(max(c.len - a.T + t + 1, 0), c.len) : c.len; }
 };
 
 // `area(v)`: 32 x D elements of LDS for wavefront v.
 template <class E, int D, int NW, class F>
 __device__ __forceinline__ void narrow_block(const Block<E, D>& k, F area, float2 (*ml)[16], int tid) {
-  const DecodeArgs& a = k.a;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), mm = lane & 15, g = lane >> 4;
   Walk<E, D, 1> w;
   w.start();
   int t_of[1];
-  k.load(w, kNarrowRows * k.rb, t_of, lane);
+  bool loaded = false;
   // the shared rows, the sequence's own, or both
 #pragma unroll 1
-  for (int own = k.shared || a.direct ? 0 : 1; own < (k.shared ? 1 : 2); ++own) {
+  for (int own = k.first_cache(); own < (k.shared ? 1 : 2); ++own) {
     const auto c = k.cache(own, kKeys);
-    const int lim[1] = {k.limit(c, own, t_of[0])};
-    w.narrow(c.K, c.V, c.kst, c.vst, c.len, lim, k.limit_all(c, own, kNarrowRows), c.from + wave, c.to, NW, a.c2, area(wave), lane);
+    w.narrow(c.K, c.V, c.kst, c.vst, c.len, c.from + wave, c.to, NW, c.c2, area(wave), lane, [&](int (&lim)[1], int& lim_all) {
+      if (!loaded) k.load(w, kNarrowRows * k.rb, t_of, lane);
+      loaded = true;
+      k.limits(c, own, kNarrowRows, t_of, lim, lim_all);
+    });
   }
   // join the wavefronts: 16 rows x D in 32 bits fill a wavefront's area; the 16-byte pieces of row r sit at piece ^ r
   __syncthreads();
@@ -504,8 +543,8 @@ __device__ __forceinline__ void narrow_block(const Block<E, D>& k, F area, float
   for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4*>(area(wave) + mm * (4 * D) + (((4 * db + g) ^ mm) << 4)) = w.o[0][db];
   if (g == 0) ml[wave][mm] = float2{w.m[0], l};
   __syncthreads();
-  const int i = tid >> 4, r = kNarrowRows * k.rb + i, d0 = (tid & 15) * (D / 16);
-  if (i >= kNarrowRows || r >= k.rows.count) return;
+  const int i = tid >> 4, d0 = (tid & 15) * (D / 16);
+  if (i >= min(kNarrowRows, k.rows.count - kNarrowRows * k.rb)) return;
   float top = -INFINITY, sum = 0.f, acc[D / 16];
 #pragma unroll
   for (int v = 0; v < NW; ++v) top = fmaxf(top, ml[v][i].x);
@@ -522,26 +561,28 @@ __device__ __forceinline__ void narrow_block(const Block<E, D>& k, F area, float
       for (int j = 0; j < 4; ++j) acc[d + j] = fmaf(f, x[j], acc[d + j]);
     }
   }
-  k.write(r, d0, acc, top, sum, (tid & 15) == 0);
+  k.write(i, d0, acc, top, sum, (tid & 15) == 0);
 }
 
 template <class E, int D>
 __device__ __forceinline__ void wide_block(const Block<E, D>& k, unsigned char* ka, unsigned char* kb, unsigned char* va, unsigned char* vb, int tid) {
-  const DecodeArgs& a = k.a;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), mm = lane & 15, g = lane >> 4;
   const int r0 = kWideRows * k.rb + 32 * wave;
   Walk<E, D, 2> w;
   int t_of[2];
-  k.load(w, r0, t_of, lane);
+  bool loaded = false;
 #pragma unroll 1
   for (int fast = 1; fast >= 0; --fast) {
     w.start();
     bool fits = true;
 #pragma unroll 1
-    for (int own = k.shared || a.direct ? 0 : 1; own < (k.shared ? 1 : 2); ++own) {
+    for (int own = k.first_cache(); own < (k.shared ? 1 : 2); ++own) {
       const auto c = k.cache(own, kWideKeys);
-      const int lim[2] = {k.limit(c, own, t_of[0]), k.limit(c, own, t_of[1])};
-      fits &= w.wide(c.K, c.V, c.kst, c.vst, c.len, lim, k.limit_all(c, own, kWideRows), c.from, c.to, a.c2, ka, kb, va, vb, wave, lane, fast);
+      fits &= w.wide(c.K, c.V, c.kst, c.vst, c.len, c.from, c.to, c.c2, ka, kb, va, vb, wave, lane, fast, [&](int (&lim)[2], int& lim_all) {
+        if (!loaded) k.load(w, r0, t_of, lane);
+        loaded = true;
+        k.limits(c, own, kWideRows, t_of, lim, lim_all);
+      });
     }
     if (!__syncthreads_or(!fits)) break;
   }
@@ -551,16 +592,17 @@ __device__ __forceinline__ void wide_block(const Block<E, D>& k, unsigned char* 
     const float sum = column_sum(w.l[cb]);
     const int r = r0 + 16 * cb + mm;
     if (r >= k.rows.count) continue;
-    int b, h, t;
-    k.rows.find(a, r, b, h, t);
-    const int z = k.rows.z;
-    const int64_t all_rows = (int64_t)a.Z * a.B * a.H * a.T, row = (((int64_t)z * a.B + b) * a.H + h) * a.T + t;
-    if (a.part_acc) {
-      float* p = a.part_acc + (k.slot * all_rows + row) * D + 4 * g;
+    if (k.acc) {
+      const uint32_t i = 32 * wave + 16 * cb + mm;
+      float* p = k.acc + (i * D + 4 * g);
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4*>(p + 16 * db) = w.o[cb][db];
-      if (g == 0) a.part_ml[k.slot * all_rows + row] = float2{w.m[cb], sum};
+      if (g == 0) k.ml[i] = float2{w.m[cb], sum};
     } else {
+      const DecodeArgs& a = kernel_args<DecodeArgs>();
+      int b, h, t;
+      k.rows.find(a, r, b, h, t);
+      const int z = k.rows.z;
       const float inv = sum == 0.f ? 0.f : 1.0f / sum;
       E* o = static_cast<E*>(a.O) + z * a.os[0] + b * a.os[1] + h * a.os[2] + t * a.os[3] + 4 * g;
 #pragma unroll
@@ -568,20 +610,22 @@ __device__ __forceinline__ void wide_block(const Block<E, D>& k, unsigned char* 
         const f32x4 x = w.o[cb][db];
         *reinterpret_cast<u32x2*>(o + 16 * db) = u32x2{pack2<E>(x[0] * inv, x[1] * inv), pack2<E>(x[2] * inv, x[3] * inv)};
       }
-      if (a.lse && g == 0) a.lse[row] = natural_lse(w.m[cb], sum);
+      if (a.lse && g == 0) a.lse[(((int64_t)z * a.B + b) * a.H + h) * a.T + t] = natural_lse(w.m[cb], sum);
     }
   }
 }
 
 // kNW: wavefronts of a workgroup (kWaves with wide blocks).
 template <class E, int D, bool kWideS, bool kWideO, int kNW>
-__global__ __launch_bounds__(64 * kNW, kWideS ? 2 : 1) void decode_kernel(const DecodeArgs a) {
+__global__ __launch_bounds__(64 * kNW, kWideS ? 2 : 1) void decode_kernel(const DecodeArgs) {
   static_assert(kNW == kWaves || !kWideS);
+  touch_args<DecodeArgs>();
+  const DecodeArgs& a = kernel_args<DecodeArgs>();
   const int tid = threadIdx.x;
   // block id -> shared units (cache, KV head, part) x row blocks, then own units (.., sequence, part) x row blocks.  Row blocks of a unit
   // read the same keys: they are given ids 8 apart, which land on one XCD at about the same time.
-  int id = blockIdx.x, in_turn, part;
-  Block<E, D> k{a};
+  int id = blockIdx.x, in_turn;
+  Block<E, D> k;
   k.shared = id < a.ids_s;
   if (!k.shared) id -= a.ids_s;
   const int turn = (k.shared ? a.by_blocks_s : a.by_blocks_o).by(id, in_turn);
@@ -591,10 +635,9 @@ __global__ __launch_bounds__(64 * kNW, kWideS ? 2 : 1) void decode_kernel(const 
   unit = a.by_Hkv.by(unit, k.rows.g);
   k.rows.b = -1;
   if (!k.shared) unit = a.by_B.by(unit, k.rows.b);
-  part = a.by_Z.by(unit, k.rows.z);
+  k.part = a.by_Z.by(unit, k.rows.z);
   k.rows.count = (k.shared ? a.B : 1) * a.T * a.G;
-  k.part = part;
-  k.slot = k.shared ? part : a.splits_s + part;
+  k.find_states(a, (k.shared ? kWideS : kWideO) ? kWideRows : kNarrowRows);
 
   constexpr int kTile = kKeys * D * 2, kWideTile = kWideKeys * D * 2;
   __shared__ float2 ml[kNW][16];
@@ -611,7 +654,7 @@ __global__ __launch_bounds__(64 * kNW, kWideS ? 2 : 1) void decode_kernel(const 
 // Joins the parts of a row: D/4 threads x `lanes` part lanes a row.
 template <class E, int D>
 __global__ __launch_bounds__(256) void decode_join_kernel(const DecodeArgs a, int parts, int lanes) {
-  constexpr int kQuads = D / 4;
+  constexpr int kQuads = D / 4, kBatch = 4;
   __shared__ f32x4 acc_s[256];
   __shared__ float2 ml_s[256];
   const int64_t all_rows = (int64_t)a.Z * a.B * a.H * a.T;
@@ -619,28 +662,35 @@ __global__ __launch_bounds__(256) void decode_join_kernel(const DecodeArgs a, in
   const int64_t row = (int64_t)blockIdx.x * (256 / per_row) + tid / per_row;
   const int pl = tid % per_row / kQuads, quad = tid % kQuads;
   const bool live = row < all_rows;
+  int t, h, b, in_group;
+  const int z = a.by_B.by(a.by_H.by(a.by_T.by((int)row, t), h), b), hk = a.by_G.by(h, in_group);
+  // the row in a shared part, and in one of its sequence's (Block::find_states)
+  const int64_t row_s = ((int64_t)z * a.Hkv + hk) * (a.B * a.T * a.G) + (t * a.B + b) * a.G + in_group;
+  const int64_t row_o = (((int64_t)z * a.B + b) * a.Hkv + hk) * (a.T * a.G) + t * a.G + in_group;
   float top = -INFINITY, sum = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   if (live) {
-    for (int p0 = pl; p0 < parts; p0 += 4 * lanes) {       // four parts' loads in flight
-      float2 s[4];
-      f32x4 v[4];
+#pragma unroll 1
+    for (int p0 = pl; p0 < parts; p0 += kBatch * lanes) {  // their loads in flight together
+      float2 s[kBatch];
+      f32x4 v[kBatch];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < kBatch; ++j) {
         const int p = min(p0 + j * lanes, parts - 1);
-        s[j] = a.part_ml[p * all_rows + row];
-        v[j] = *reinterpret_cast<const f32x4*>(a.part_acc + (p * all_rows + row) * D + 4 * quad);
+        const int64_t i = p * all_rows + (p < a.splits_s ? row_s : row_o);
+        s[j] = a.part_ml[i];
+        v[j] = *reinterpret_cast<const f32x4*>(a.part_acc + i * D + 4 * quad);
       }
       float next = top;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) next = fmaxf(next, s[j].x);
+      for (int j = 0; j < kBatch; ++j) next = fmaxf(next, s[j].x);
       const float f0 = part_weight(top, next);
       top = next;
       sum *= f0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[i] *= f0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < kBatch; ++j) {
         if (p0 + j * lanes < parts) {
           const float f = part_weight(s[j].x, top);
           sum = fmaf(f, s[j].y, sum);
@@ -655,9 +705,11 @@ __global__ __launch_bounds__(256) void decode_join_kernel(const DecodeArgs a, in
     ml_s[tid] = float2{top, sum};
     __syncthreads();
     if (pl != 0) return;
+#pragma unroll 1
     for (int p = 1; p < lanes; ++p) top = fmaxf(top, ml_s[tid + p * kQuads].x);
     sum = 0.f;
     acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
     for (int p = 0; p < lanes; ++p) {
       const float f = part_weight(ml_s[tid + p * kQuads].x, top);
       sum = fmaf(f, ml_s[tid + p * kQuads].y, sum);
@@ -666,8 +718,6 @@ __global__ __launch_bounds__(256) void decode_join_kernel(const DecodeArgs a, in
     }
   }
   if (!live) return;
-  int t, h, b;
-  const int z = a.by_B.by(a.by_H.by(a.by_T.by((int)row, t), h), b);
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
   E* o = static_cast<E*>(a.O) + z * a.os[0] + b * a.os[1] + h * a.os[2] + t * a.os[3] + 4 * quad;
   *reinterpret_cast<u32x2*>(o) = u32x2{pack2<E>(acc[0] * inv, acc[1] * inv), pack2<E>(acc[2] * inv, acc[3] * inv)};
@@ -701,8 +751,9 @@ Shape shape_of(const DecodeArgs& a) {
     return s;
   }
   s.direct = false;
-  // One round of workgroups with the same number of keys each, 128 at least
-  const int64_t keys = (units_s * a.L + (a.Lo ? units_o * a.Lo : 0)) / slots;
+  // One round of workgroups with the same number of keys each, 128 at least.  Own keys count half where the shared ones are read for several
+  // row blocks and wait for the matrix cores, not for memory (64 sequences on 128K keys 182 us, else 188; 200 on 16K 126 and 149).
+  const int64_t keys = (units_s * a.L + units_o * a.Lo / (s.blocks_s > 1 ? 2 : 1)) / slots;
   auto split = [&](int64_t len) { return (int)(len == 0 ? 0 : len / (keys > 128 ? keys : 128) > 1 ? len / (keys > 128 ? keys : 128) : 1); };
   s.splits_s = split(a.L);
   s.splits_o = split(a.Lo);
@@ -715,8 +766,10 @@ hipError_t launch(DecodeArgs a, const Shape& s, hipStream_t stream) {
   const int64_t units_s = (int64_t)a.Z * a.Hkv * s.splits_s, units_o = (int64_t)a.Z * a.Hkv * a.B * s.splits_o;
   const int64_t ids_s = (units_s + 7) / 8 * 8 * s.blocks_s, ids_o = (units_o + 7) / 8 * 8 * s.blocks_o;
   if (ids_s + ids_o <= 0 || ids_s + ids_o > 0x7fffffff) return hipErrorInvalidValue;
+  a.rows = all_rows;
   a.units_s = (int)units_s; a.units_o = (int)units_o; a.ids_s = (int)ids_s;
   a.by_blocks_s = Divisor(8 * s.blocks_s); a.by_blocks_o = Divisor(8 * s.blocks_o);
+  a.by_splits_s = Divisor(s.splits_s); a.by_splits_o = Divisor(s.splits_o);
   a.by_Z = Divisor(a.Z); a.by_B = Divisor(a.B); a.by_H = Divisor(a.H); a.by_Hkv = Divisor(a.Hkv);
   a.by_G = Divisor(a.G); a.by_BG = Divisor(a.B * a.G); a.by_T = Divisor(a.T);
   if (s.parts() == 1) a.part_acc = nullptr;                // nothing to join

@@ -128,8 +128,9 @@ struct DecodeArgs {
   float* part_acc;
   float2* part_ml;
   int blocks_s, splits_s, blocks_o, splits_o, direct;
+  int64_t rows;                  // Z * B * H * T
   int units_s, units_o, ids_s;   // (cache, KV head, part) and (.., sequence, part); block ids of shared row blocks
-  Divisor by_blocks_s, by_blocks_o, by_Z, by_B, by_H, by_Hkv, by_G, by_BG, by_T;   // (by_blocks: eight units' blocks)
+  Divisor by_blocks_s, by_blocks_o, by_splits_s, by_splits_o, by_Z, by_B, by_H, by_Hkv, by_G, by_BG, by_T;   // (by_blocks: eight units' blocks)
 };
 size_t decode_scratch_bytes(const DecodeArgs& a);
 hipError_t launch_decode(DecodeArgs a, void* scratch, hipStream_t stream);
