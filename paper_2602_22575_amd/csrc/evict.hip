@@ -130,11 +130,13 @@ __device__ __forceinline__ void list_rows(int32_t* list, int from, uint64_t sure
 }
 
 __global__ __launch_bounds__(256) void clear_kernel(const EvictArgs a) {
+  touch_args<EvictArgs>();
   const Scratch s(a, blockIdx.x);
   for (int i = threadIdx.x; i < Scratch::kHead; i += 256) s.counts[i] = 0;
 }
 
 __global__ __launch_bounds__(kT) void count_kernel(const EvictArgs a) {
+  touch_args<EvictArgs>();
   __shared__ uint32_t counts[kBins];
   const int tid = threadIdx.x;
   const int stretch = (int)(blockIdx.x % stretches(a.L));
@@ -159,6 +161,7 @@ __global__ __launch_bounds__(kT) void count_kernel(const EvictArgs a) {
 }
 
 __global__ __launch_bounds__(kT) void collect_kernel(const EvictArgs a) {
+  touch_args<EvictArgs>();
   __shared__ int2 part[kWaves];
   __shared__ Bin found;
   __shared__ uint32_t base;
@@ -203,6 +206,7 @@ __global__ __launch_bounds__(kT) void collect_kernel(const EvictArgs a) {
 }
 
 __global__ __launch_bounds__(kT) void list_kernel(const EvictArgs a) {
+  touch_args<EvictArgs>();
   __shared__ uint32_t counts[kBins], room[kRoom];
   __shared__ int2 part[kWaves];
   __shared__ Bin found;
@@ -279,6 +283,7 @@ __global__ __launch_bounds__(kT) void list_kernel(const EvictArgs a) {
 // kRows: of a head at most.
 template <int kRows>
 __global__ __launch_bounds__(kT) void select_kernel(const EvictArgs a) {
+  touch_args<EvictArgs>();
   __shared__ __attribute__((aligned(16))) uint32_t keys[kRows];   // 0: a row that does not compete (the least key is 0x7fffff)
   __shared__ uint32_t counts[kBins];
   __shared__ int2 part[kWaves];
@@ -353,6 +358,7 @@ __global__ __launch_bounds__(kT) void select_kernel(const EvictArgs a) {
 // Rows of 2 * D bytes, D / 8 lanes a row, kEach of them a thread; blockIdx.y: K and the weights, or V.
 template <int D, int kEach>
 __global__ __launch_bounds__(256) void gather_kernel(const EvictArgs a, int chunks) {
+  touch_args<EvictArgs>();
   constexpr int kLanes = D / 8, kStep = 256 / kLanes;
   const int64_t head = blockIdx.x / chunks;
   const int z = (int)(head / a.Hkv), hk = (int)(head % a.Hkv), lane = threadIdx.x % kLanes;

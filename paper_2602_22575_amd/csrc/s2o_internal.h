@@ -149,6 +149,7 @@ struct WeightsArgs {
   float2* stats;         // [key part][cache, KV head][row]: {reference, sum}, joined: {reference, 1 / sum}
   float* sums;           // [row part][cache, KV head][key]
   int row_blocks, key_parts, ranges, range_tiles, row_parts;
+  Divisor by_Z, by_Hkv, by_G, by_BG, by_key_parts, by_row_parts;
 };
 size_t weights_scratch_bytes(WeightsArgs a, bool given);
 hipError_t launch_weights(WeightsArgs a, void* scratch, hipStream_t stream);

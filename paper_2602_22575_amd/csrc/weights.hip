@@ -27,17 +27,25 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves, kTileRows = 64;
 // fewer rows 2 or 1, so that all four wavefronts have some.
 template <int CB>
 constexpr int kRowsWg = 16 * CB * kWaves;
+constexpr int kFewParts = 4;                       // parts of a row's statistics that its readers join themselves
 constexpr int kRange = 32;                         // tiles of keys of a workgroup of sum_kernel at most
 
 struct RowOf {
   int t, b, g;
   __device__ __forceinline__ void set(const WeightsArgs& a, int r) {
-    const int per_t = a.B * a.G, rest = r % per_t;
-    t = r / per_t;
-    b = rest / a.G;
-    g = rest % a.G;
+    int rest;
+    t = a.by_BG.by(r, rest);
+    b = a.by_G.by(rest, g);
   }
 };
+
+// Of `all` things in parts (by_parts), those of one part: as many for each, or one more in the first parts.
+__device__ __forceinline__ void share(const Divisor& by_parts, int all, int part, int& from, int& to) {
+  int more;
+  const int each = by_parts.by(all, more);
+  from = part * each + min(part, more);
+  to = from + each + (part < more);
+}
 
 // Keys that query token t sees.
 __device__ __forceinline__ int row_limit(const WeightsArgs& a, int len, int t) { return a.causal ? min(max(len - a.T + t + 1, 0), len) : len; }
@@ -60,8 +68,8 @@ __device__ __forceinline__ void order_tile() {
   __builtin_amdgcn_sched_group_barrier(0x402, 12 * CB, 0);
 }
 
-// Streams tiles from .. to - 1 of 64 keys through four LDS buffers, three tiles ahead of the one that is worked on: two workgroups a CU
-// then have 96 KB on their way (with one tile ahead the kernels waited for memory: 81 and 84 us for 128K keys of 8 heads).  All threads of
+// Streams tiles from .. to - 1 of 64 keys through three LDS buffers, two tiles ahead of the one that is worked on: two workgroups a CU
+// then have 64 KB on their way (with one tile ahead the kernels waited for memory).  All threads of
 // the workgroup; fast(t, tile) or, where it returns false, any(t, tile) works on tile t; the buffers are separate arrays, so
 // that the compiler sees that reads of one need not wait for the loads that fill another.
 template <class E, int D, class F, class G>
@@ -172,6 +180,11 @@ struct Stats {
   }
 };
 
+// (Nothing seen: a reference and factor that make every weight zero.)
+__device__ __forceinline__ float2 joined(float top, float sum) {
+  return sum == 0.f ? float2{INFINITY, 0.f} : float2{top == -INFINITY ? 0.f : top, 1.0f / sum};
+}
+
 template <class E, int D, int CB>
 __global__ __launch_bounds__(kThreads, 3) void stats_kernel(const WeightsArgs a) {
   constexpr int kTile = kTileRows * D * 2;
@@ -179,12 +192,9 @@ __global__ __launch_bounds__(kThreads, 3) void stats_kernel(const WeightsArgs a)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int mm = lane & 15, g = lane >> 4;
   // the row blocks that see the most keys first
-  int id = blockIdx.x;
-  const int hk = id % a.Hkv;
-  id /= a.Hkv;
-  const int z = id % a.Z;
-  id /= a.Z;
-  const int part = id % a.key_parts, rb = a.row_blocks - 1 - id / a.key_parts;
+  touch_args<WeightsArgs>();
+  int hk, z, part;
+  const int rb = a.row_blocks - 1 - a.by_key_parts.by(a.by_Z.by(a.by_Hkv.by(blockIdx.x, hk), z), part);
   const int R = a.B * a.T * a.G, len = filled(a.lens, z, a.L);
   const E* Q = static_cast<const E*>(a.Q) + z * a.qs[0];
   const E* K = static_cast<const E*>(a.K) + z * a.ks[0] + hk * a.ks[1];
@@ -207,7 +217,8 @@ __global__ __launch_bounds__(kThreads, 3) void stats_kernel(const WeightsArgs a)
   const int full = row_limit(a, len, row.t) / kTileRows;
   row.set(a, min((rb + 1) * kRowsWg<CB>, R) - 1);
   const int tiles = (row_limit(a, len, row.t) + kTileRows - 1) / kTileRows;
-  const int from = (int)((int64_t)tiles * part / a.key_parts), to = (int)((int64_t)tiles * (part + 1) / a.key_parts);
+  int from, to;
+  share(a.by_key_parts, tiles, part, from, to);
   const bool active = rb * kRowsWg<CB> + wave * 16 * CB < R;     // the wavefront has rows at all
 
   stream_keys<E, D>(K, a.ks[2], len, from, to, b0, b1, b2, tid,
@@ -217,18 +228,17 @@ __global__ __launch_bounds__(kThreads, 3) void stats_kernel(const WeightsArgs a)
   const int64_t rows = (int64_t)a.Z * a.Hkv * R;
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) {
-    const float top = column_max(w.m[cb]), ref = top == -INFINITY ? 0.f : top;
-    const float sum = column_sum(w.l[cb] * exp2_(w.m[cb] - ref));
+    const float top = column_max(w.m[cb]);
+    const float sum = column_sum(w.l[cb] * exp2_(w.m[cb] - (top == -INFINITY ? 0.f : top)));
     const int r = rb * kRowsWg<CB> + wave * 16 * CB + 16 * cb + mm;
     if (g == 0 && r < R) {
       const int64_t i = ((int64_t)z * a.Hkv + hk) * R + r;
-      // (nothing seen: a reference and factor that make every weight zero)
-      a.stats[part * rows + i] = a.key_parts > 1 ? float2{top, sum} : sum == 0.f ? float2{INFINITY, 0.f} : float2{ref, 1.0f / sum};
+      a.stats[part * rows + i] = a.key_parts > 1 ? float2{top, sum} : joined(top, sum);
     }
   }
 }
 
-// Sixteen rows a workgroup, sixteen lanes a row.
+// Joins the statistics of a row's parts where they are more than kFewParts: sixteen rows a workgroup, sixteen lanes a row.
 __global__ __launch_bounds__(256) void stats_join_kernel(float2* stats, int64_t rows, int parts) {
   const int64_t i = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
   const int lane = threadIdx.x % 16;
@@ -249,7 +259,7 @@ __global__ __launch_bounds__(256) void stats_join_kernel(float2* stats, int64_t 
   sum *= exp2_(top - ref);
 #pragma unroll
   for (int d = 1; d < 16; d *= 2) sum += __shfl_xor(sum, d);
-  if (i < rows && lane == 0) stats[i] = sum == 0.f ? float2{INFINITY, 0.f} : float2{ref, 1.0f / sum};
+  if (i < rows && lane == 0) stats[i] = joined(all, sum);
 }
 
 // ---- the weights
@@ -258,7 +268,8 @@ __global__ __launch_bounds__(256) void stats_join_kernel(float2* stats, int64_t 
 // A side, so that a lane of an accumulator block is a key and its registers are rows: a key's terms are added up inside the lane.  A tile's sums of the four
 // wavefronts meet in LDS and add to the range's.
 template <class E, int D, int CB, bool kGiven>
-__global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs) {
+  const WeightsArgs& a = kernel_args<WeightsArgs>();
   typedef typename Vec<E>::x8 x8;
   constexpr int kTile = kTileRows * D * 2;
   __shared__ __attribute__((aligned(256))) unsigned char b0[kTile], b1[kTile], b2[kTile];
@@ -268,12 +279,10 @@ __global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int mm = lane & 15, g = lane >> 4;
   // the ranges and the row blocks with the most work first: the first keys, the last rows
-  int id = blockIdx.x;
-  const int hk = id % a.Hkv;
-  id /= a.Hkv;
-  const int z = id % a.Z;
-  id /= a.Z;
-  const int part = a.row_parts - 1 - id % a.row_parts, range = id / a.row_parts;
+  touch_args<WeightsArgs>();
+  int hk, z, part;
+  const int range = a.by_row_parts.by(a.by_Z.by(a.by_Hkv.by(blockIdx.x, hk), z), part);
+  part = a.row_parts - 1 - part;
   const int R = a.B * a.T * a.G, len = filled(a.lens, z, a.L);
   const int t0 = range * a.range_tiles, t1 = min(t0 + a.range_tiles, (len + kTileRows - 1) / kTileRows);
   if (t0 >= t1) return;                            // (uniform: entries behind the cache's end stay as they are)
@@ -291,8 +300,10 @@ __global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs a) {
       range_s[(t - t0) * kTileRows + lane] += x;
     }
   };
-  const int rb0 = (int)((int64_t)a.row_blocks * part / a.row_parts), rb1 = (int)((int64_t)a.row_blocks * (part + 1) / a.row_parts);
+  int rb0, rb1;
+  share(a.by_row_parts, a.row_blocks, part, rb0, rb1);
   for (int rb = rb0; rb < rb1; ++rb) {
+    const WeightsArgs& a = kernel_args<WeightsArgs>();
     RowOf row;
     row.set(a, min((rb + 1) * kRowsWg<CB>, R) - 1);
     const int end = min(t1, (row_limit(a, len, row.t) + kTileRows - 1) / kTileRows);   // tiles that the block's last row sees
@@ -322,9 +333,22 @@ __global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs a) {
           my_inv = exp2_(-(fmaf(x, a.l2e_hi, -my_ref) + x * a.l2e_lo));
         }
       } else {
-        const float2 s = a.stats[head * R + r0 + lane];
-        my_ref = s.x;
-        my_inv = s.y;
+        const int64_t rows = (int64_t)a.Z * a.Hkv * R, i = head * R + r0 + lane;
+        const bool one = a.key_parts == 1 || a.key_parts > kFewParts;      // what the launches before have made of them
+        float2 s[kFewParts];
+#pragma unroll
+        for (int p = 0; p < kFewParts; ++p) s[p] = a.stats[(one ? 0 : min(p, a.key_parts - 1)) * rows + i];
+        if (!one) {
+          float top = -INFINITY, l = 0.f;
+#pragma unroll
+          for (int p = 0; p < kFewParts; ++p) top = fmaxf(top, s[p].x);
+#pragma unroll
+          for (int p = 0; p < kFewParts; ++p)
+            if (p < a.key_parts) l = fmaf(s[p].y, exp2_(s[p].x - (top == -INFINITY ? 0.f : top)), l);
+          s[0] = joined(top, l);
+        }
+        my_ref = s[0].x;
+        my_inv = s[0].y;
       }
     }
     wave_fence();
@@ -403,10 +427,11 @@ __global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs a) {
     __syncthreads();                               // (tile and sums' buffers are free again)
   }
   __syncthreads();
+  const WeightsArgs& e = kernel_args<WeightsArgs>();
   const int key = t0 * kTileRows;
   for (int i = tid; i < min((t1 - t0) * kTileRows, len - key); i += kThreads) {
-    if (a.row_parts > 1) a.sums[((int64_t)part * a.Z * a.Hkv + head) * a.L + key + i] = range_s[i];
-    else a.out[head * a.L + key + i] = a.prev ? a.prev[head * a.L + key + i] + range_s[i] : range_s[i];
+    if (e.row_parts > 1) e.sums[((int64_t)part * e.Z * e.Hkv + head) * e.L + key + i] = range_s[i];
+    else e.out[head * e.L + key + i] = e.prev ? e.prev[head * e.L + key + i] + range_s[i] : range_s[i];
   }
 }
 
@@ -453,7 +478,9 @@ size_t stats_bytes(const WeightsArgs& a) {
 }
 
 template <class E, int D, int CB>
-hipError_t launch(const WeightsArgs& a, hipStream_t stream) {
+hipError_t launch(WeightsArgs a, hipStream_t stream) {
+  a.by_Z = Divisor(a.Z); a.by_Hkv = Divisor(a.Hkv); a.by_G = Divisor(a.G); a.by_BG = Divisor(a.B * a.G);
+  a.by_key_parts = Divisor(a.key_parts); a.by_row_parts = Divisor(a.row_parts);
   const int64_t heads = (int64_t)a.Z * a.Hkv, rows = heads * a.B * a.T * a.G;
   const int64_t sum_blocks = heads * a.row_parts * a.ranges;
   if (sum_blocks > 0x7fffffff) return hipErrorInvalidValue;
@@ -463,7 +490,7 @@ hipError_t launch(const WeightsArgs& a, hipStream_t stream) {
     const int64_t blocks = heads * a.row_blocks * a.key_parts;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     hipLaunchKernelGGL((stats_kernel<E, D, CB>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
-    if (a.key_parts > 1)
+    if (a.key_parts > kFewParts)
       hipLaunchKernelGGL(stats_join_kernel, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, a.stats, rows, a.key_parts);
     hipLaunchKernelGGL((sum_kernel<E, D, CB, false>), dim3((unsigned)sum_blocks), dim3(kThreads), 0, stream, a);
   }
