@@ -213,6 +213,7 @@ int s2o_attention_prefix(const void* Q, const void* K, const void* V, const s2o_
  *   - `lens` arrays (int32, device) say how many rows of a cache are filled; NULL: all that `cache_len` (`own_len`) counts.
  *     They are read by the kernels, so a captured call follows them; values outside [0, cache_len] are clamped.
  *     Rows behind them are never read into a result, whatever they hold;
+ *   - outputs and scratch must not overlap the inputs or each other (S2O_EINVAL where the ranges that they span do);
  *   - the calls can be captured from the first one on (they set no kernel attributes). */
 enum { S2O_BF16 = 0, S2O_F16 = 1 };
 
@@ -307,8 +308,7 @@ int s2o_evict_sizes(const s2o_evict_params* params, size_t* scratch_bytes);
  *   K_out,V_out [Z,Hkv,keep,D]: their rows (K and K_out, or V and V_out, may both be NULL: nothing is moved)
  *   weights_out [Z,Hkv,keep] fp32: their weights, or NULL
  *   lens_out    [Z] int32: m, or NULL
- * Entries behind m are left as they were.  The outputs must not overlap the inputs or each other (S2O_EINVAL where the ranges that they
- * span do).  scratch as above. */
+ * Entries behind m are left as they were.  scratch as above. */
 int s2o_evict(const void* K, const void* V, const float* weights, const int32_t* lens, const s2o_evict_params* params, void* K_out,
               void* V_out, float* weights_out, int32_t* kept, int32_t* lens_out, void* scratch, size_t scratch_bytes, void* stream);
 

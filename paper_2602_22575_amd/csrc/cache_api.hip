@@ -80,6 +80,15 @@ struct Range {
   }
 };
 
+// What is written to overlaps nothing that is read and nothing else that is written.
+int check_apart(std::initializer_list<Range> outs, std::initializer_list<Range> ins) {
+  for (const Range& o : outs) {
+    for (const Range& i : ins) if (o.meets(i)) return S2O_EINVAL;
+    for (const Range& p : outs) if (&p != &o && o.meets(p)) return S2O_EINVAL;
+  }
+  return S2O_OK;
+}
+
 int check_heads(int Z, int B, int H, int Hkv, int D, int T, int dtype, float scale) {
   if (Z <= 0 || B <= 0 || H <= 0 || Hkv <= 0 || D <= 0 || T <= 0) return S2O_EINVAL;
   if (H % Hkv != 0) return S2O_EINVAL;
@@ -182,7 +191,13 @@ int s2o_decode(const void* Q, const void* K, const void* V, const void* own_K, c
   if (!Q || !O || (a.L && (!K || !V)) || (a.Lo && (!own_K || !own_V))) return S2O_EINVAL;
   if (misaligned(Q, 16) || misaligned(O, 16) || misaligned(lse, 4) || misaligned(lens, 4) || misaligned(own_lens, 4)) return S2O_EINVAL;
   if ((a.L && (misaligned(K, 16) || misaligned(V, 16))) || (a.Lo && (misaligned(own_K, 16) || misaligned(own_V, 16)))) return S2O_EINVAL;
-  CHECK(check_scratch(scratch, scratch_bytes, s2o::decode_scratch_bytes(a)));
+  const size_t need = s2o::decode_scratch_bytes(a);
+  CHECK(check_scratch(scratch, scratch_bytes, need));
+  const int64_t q[4] = {a.Z, a.B, a.H, a.T}, k[3] = {a.Z, a.Hkv, a.L}, o[4] = {a.Z, a.B, a.Hkv, a.Lo};
+  const size_t kb = a.L ? 1 : 0, ob = a.Lo ? 1 : 0, seqs = (size_t)a.Z * a.B;
+  CHECK(check_apart({{O, span(a.os, q, 4, a.D)}, {lse, seqs * a.H * a.T * 4}, {scratch, need}},
+                    {{Q, span(a.qs, q, 4, a.D)}, {K, kb * span(a.ks, k, 3, a.D)}, {V, kb * span(a.vs, k, 3, a.D)}, {own_K, ob * span(a.oks, o, 4, a.D)},
+                     {own_V, ob * span(a.ovs, o, 4, a.D)}, {lens, (size_t)a.Z * 4}, {own_lens, seqs * 4}}));
   a.Q = Q; a.K = K; a.V = V; a.oK = own_K; a.oV = own_V;
   a.lens = lens; a.own_lens = own_lens; a.O = O; a.lse = lse;
   return done(s2o::launch_decode(a, scratch, (hipStream_t)stream));
@@ -205,7 +220,12 @@ int s2o_key_weights(const void* Q, const void* K, const float* lse, const int32_
     return S2O_EINVAL;
   const size_t bytes = (size_t)a.Z * a.Hkv * a.L * 4;
   if (prev != weights && Range{prev, bytes}.meets({weights, bytes})) return S2O_EINVAL;
-  CHECK(check_scratch(scratch, scratch_bytes, s2o::weights_scratch_bytes(a, lse != nullptr)));
+  const size_t need = s2o::weights_scratch_bytes(a, lse != nullptr);
+  CHECK(check_scratch(scratch, scratch_bytes, need));
+  const int64_t q[4] = {a.Z, a.B, a.H, a.T}, k[3] = {a.Z, a.Hkv, a.L};
+  CHECK(check_apart({{weights, bytes}, {scratch, need}},
+                    {{Q, span(a.qs, q, 4, a.D)}, {K, span(a.ks, k, 3, a.D)}, {lse, (size_t)a.Z * a.B * a.H * a.T * 4}, {lens, (size_t)a.Z * 4}}));
+  CHECK(check_apart({{scratch, need}}, {{prev, bytes}}));
   a.Q = Q; a.K = K; a.lse = lse; a.lens = lens; a.prev = prev; a.out = weights;
   return done(s2o::launch_weights(a, scratch, (hipStream_t)stream));
 }
@@ -225,15 +245,11 @@ int s2o_evict(const void* K, const void* V, const float* weights, const int32_t*
   if (misaligned(K, 16) || misaligned(V, 16) || misaligned(K_out, 16) || misaligned(V_out, 16)) return S2O_EINVAL;
   if (misaligned(weights, 4) || misaligned(lens, 4) || misaligned(weights_out, 4) || misaligned(kept, 4) || misaligned(lens_out, 4)) return S2O_EINVAL;
   const int64_t in[3] = {a.Z, a.Hkv, a.L}, out[3] = {a.Z, a.Hkv, a.keep};
-  const size_t heads = (size_t)a.Z * a.Hkv;
-  const Range ins[] = {{K, span(a.ks, in, 3, a.D)}, {V, span(a.vs, in, 3, a.D)}, {weights, heads * a.L * 4}, {lens, (size_t)a.Z * 4}};
-  const Range outs[] = {{K_out, span(a.kos, out, 3, a.D)}, {V_out, span(a.vos, out, 3, a.D)}, {weights_out, heads * a.keep * 4},
-                        {kept, heads * a.keep * 4}, {lens_out, (size_t)a.Z * 4}};
-  for (const Range& o : outs) {
-    for (const Range& i : ins) if (o.meets(i)) return S2O_EINVAL;
-    for (const Range& p : outs) if (&p != &o && o.meets(p)) return S2O_EINVAL;
-  }
-  CHECK(check_scratch(scratch, scratch_bytes, s2o::evict_scratch_bytes(a)));
+  const size_t heads = (size_t)a.Z * a.Hkv, need = s2o::evict_scratch_bytes(a);
+  CHECK(check_apart({{K_out, span(a.kos, out, 3, a.D)}, {V_out, span(a.vos, out, 3, a.D)}, {weights_out, heads * a.keep * 4}, {kept, heads * a.keep * 4},
+                     {lens_out, (size_t)a.Z * 4}, {scratch, need}},
+                    {{K, span(a.ks, in, 3, a.D)}, {V, span(a.vs, in, 3, a.D)}, {weights, heads * a.L * 4}, {lens, (size_t)a.Z * 4}}));
+  CHECK(check_scratch(scratch, scratch_bytes, need));
   a.K = K; a.V = V; a.weights = weights; a.lens = lens;
   a.K_out = K_out; a.V_out = V_out; a.weights_out = weights_out; a.kept = kept; a.lens_out = lens_out;
   return done(s2o::launch_evict(a, scratch, (hipStream_t)stream));

@@ -212,3 +212,39 @@ def test_other_device_and_stream(monkeypatch):
     assert b._on_device(torch.device("cuda:0"), _S("cuda:0", 0x80)) == (0x80, None)
     with pytest.raises(ValueError, match="stream"):
         b._on_device(torch.device("cuda:0"), _S("cuda:1", 0x80))
+
+
+# ---- outputs and scratch on top of something else
+def _spread(n):
+    return [C.c_void_p((i + 1) << 28) for i in range(n)]
+
+
+def test_decode_refuses_overlaps(lib):
+    p = b.make_decode_params(2, 3, 4, 2, 128, 1, 5000, 10)
+    at = _spread(10)
+    need = b.s2o_decode_sizes(p)["scratch"]
+    args = at[:7] + [C.byref(p), at[7], at[8], at[9], need, None]
+    cases = [(8, at[i], b.S2O_EINVAL) for i in range(7)] + [(9, at[i], b.S2O_EINVAL) for i in range(8)] + [(10, at[i], b.S2O_EINVAL) for i in range(9)]
+    q = 2 * 3 * 4 * 128 * 2                                                          # the last bytes of Q, of O, of K
+    cases += [(8, C.c_void_p(at[0].value + q - 16), b.S2O_EINVAL), (9, C.c_void_p(at[7].value + q - 4), b.S2O_EINVAL),
+              (8, C.c_void_p(at[1].value + 2 * 2 * 5000 * 256 - 16), b.S2O_EINVAL), (10, C.c_void_p(at[8].value - 256), b.S2O_EINVAL)]
+    _refused(lib.s2o_decode, args, cases)
+
+
+def test_weights_refuse_overlaps(lib):
+    p = b.make_weights_params(1, 1, 4, 2, 128, 64, 10000, causal=1)
+    at = _spread(7)
+    need = b.s2o_key_weights_sizes(p)["scratch"]
+    # Q K lse lens params prev weights scratch
+    args = at[:4] + [C.byref(p), at[4], at[5], at[6], need, None]
+    _refused(lib.s2o_key_weights, args, [(6, at[i], b.S2O_EINVAL) for i in range(4)] + [(6, C.c_void_p(at[4].value + 4), b.S2O_EINVAL)])
+    args[2] = None                                                                   # (it needs scratch then)
+    _refused(lib.s2o_key_weights, args, [(7, at[i], b.S2O_EINVAL) for i in (0, 1, 3, 4, 5)] + [(6, C.c_void_p(at[6].value + need - 4), b.S2O_EINVAL)])
+
+
+def test_evict_refuses_scratch_on_top_of_an_output(lib):
+    p = b.make_evict_params(1, 2, 128, 100000, 100)
+    at = _spread(10)
+    need = b.s2o_evict_sizes(p)["scratch"]
+    args = at[:4] + [C.byref(p)] + at[4:9] + [at[9], need, None]
+    _refused(lib.s2o_evict, args, [(10, x, b.S2O_EINVAL) for x in at[:9]])
