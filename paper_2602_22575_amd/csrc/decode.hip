@@ -234,7 +234,7 @@ struct Walk {
   // The first 16 keys find the references, the last tiles may have hidden keys.  For the others, if `fast`, a tile's products and exponentials
   // are one straight run of instructions, its second half's exponentials behind its first half's products: numerators are formed
   // against the references as they are, and a reference moves afterwards, where a tile's sum has outgrown 2^10.  Returns false where a numerator
-  // may have outgrown the element type on the way: all of it is to be done again, not fast.
+  // or an accumulator may have outgrown its type on the way: all of it is to be done again, not fast.
   template <class F>
   __device__ __forceinline__ bool wide(const E* K, const E* V, int64_t kstride, int64_t vstride, int len, int from, int to, float c2,
                                        unsigned char* ka, unsigned char* kb_, unsigned char* va, unsigned char* vb, int wave, int lane,
@@ -403,7 +403,15 @@ struct Walk {
       const bool odd = (t - from) & 1;
       any_tile(t, odd ? kb_ : ka, odd ? vb : va, odd ? ka : kb_, odd ? va : vb);
     }
-    return fits;
+    // (values near the end of the 32-bit range, times numerators far above 1)
+    float rest = 0.f;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rest = fmaf(o[cb][db][i], 0.f, rest);
+    return fits && __builtin_amdgcn_ballot_w64(!(rest == 0.f)) == 0;
   }
 };
 
@@ -584,7 +592,7 @@ __device__ __forceinline__ void wide_block(const Block<E, D>& k, unsigned char* 
         k.limits(c, own, kWideRows, t_of, lim, lim_all);
       });
     }
-    if (!__syncthreads_or(!fits)) break;
+    if (!fast || !__syncthreads_or(!fits)) break;
   }
   // O^T to rows: lane l's piece of row l % 16 is dims 16 * db + 4 * g .. + 3
 #pragma unroll

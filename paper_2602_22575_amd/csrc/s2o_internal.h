@@ -98,18 +98,20 @@ int hip_fail(hipError_t e);
 
 // Quotient and rest of non-negative numbers below 2^31 by d = 1 .. 2^31 - 1 that the host has prepared: a product's upper half instead of the
 // forty instructions of a division.  mul = ceil(2^(31 + s) / d), 2^(s-1) < d <= 2^s: n * mul / 2^(31 + s) is off by less than 1/d above.
-struct Divisor {
-  uint32_t mul, shift, d;
+// Laid out to be loaded in one piece.
+struct alignas(16) Divisor {
+  uint32_t mul, shift, d, whole;   // whole: all bits set where d = 1, whose mul has no room
   Divisor() = default;
-  __host__ explicit Divisor(uint32_t d_) : mul(0), shift(0), d(d_) {
+  __host__ explicit Divisor(uint32_t d_) : mul(0), shift(0), d(d_), whole(~0u) {
     if (d <= 1) return;
     uint32_t s = 0;
     while ((1ull << s) < d) ++s;
     mul = (uint32_t)(((1ull << (31 + s)) + d - 1) / d);
     shift = s - 1;
+    whole = 0;
   }
   __device__ __forceinline__ int by(int n, int& rest) const {
-    const uint32_t q = mul ? __umulhi((uint32_t)n, mul) >> shift : (uint32_t)n;
+    const uint32_t q = (__umulhi((uint32_t)n, mul) + ((uint32_t)n & whole)) >> shift;
     rest = n - (int)(q * d);
     return (int)q;
   }

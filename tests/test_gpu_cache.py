@@ -155,6 +155,83 @@ def test_decode_bad_values_where_nobody_looks(dt, L, own):
     assert torch.isfinite(O[1, 1, h:, :T - 1]).all() and torch.equal(lse[1, 1, h:, :T - 1], clean[1][1, 1, h:, :T - 1])
 
 
+# Scores are set by the first element of the keys, in steps of the exponent: with Q's first element 8 and a scale of 1/8 a key's score is
+# its own first element.
+def _scored(x, Z, B, H, Hkv, D, dt, seed, gain=0.0):
+    """Q, K, V with scores x [L] (rounded to the type) and a little more (gain)."""
+    g = _gen(seed)
+    L = len(x)
+    Q = u.randn(g, Z, B, H, 1, D, dtype=dt, gain=gain)
+    K, V = u.randn(g, Z, Hkv, L, D, dtype=dt, gain=gain), u.randn(g, Z, Hkv, L, D, dtype=dt)
+    Q[..., 0] = 8.0
+    K[..., 0] = torch.as_tensor(x, device="cuda:0").to(u.DTYPES[dt])
+    return Q, K, V
+
+
+def _steps(kind, L):
+    x = np.zeros(L)
+    i = np.arange(L)
+    if kind == "one far above":                  # in the middle of a tile of 64 keys, more than any numerator's room above the others
+        x[L // 2 + 5] = 100.0
+    elif kind == "rising":                       # references move in nearly every tile
+        x = i * (90.0 / L)
+    elif kind == "falling":
+        x = -i * (90.0 / L)
+    elif kind == "first unseen":                 # the first keys' scores are -infinity: no reference there
+        x[:70] = -np.inf
+    elif kind == "every other unseen":
+        x[::2] = -np.inf
+    elif kind == "few jumps":
+        x[i % 97 == 50] = 14.0
+        x[i % 389 == 100] = 30.0
+    return x
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("D,B", [(64, 40), (128, 40), (128, 3)])                     # 160 rows on a KV head, and 12
+@pytest.mark.parametrize("kind", ["one far above", "rising", "falling", "first unseen", "every other unseen", "few jumps"])
+def test_decode_scores_far_apart(kind, D, B, dt):
+    L = 1500
+    Q, K, V = _scored(_steps(kind, L), 1, B, 8, 2, D, dt, seed=31, gain=0.25)
+    p = s2o.make_decode_params(1, B, 8, 2, D, 1, L, dtype=dt, softmax_scale=0.125)
+    Q = Q.abs()                                                                      # (no -1 * -inf)
+    got = run_decode((Q, K, V, None, None), p)
+    O, lse = (_f(t) for t in got)
+    q, k, v = _f(Q), _f(K), _f(V)
+    ref, ref_lse, A = u.decode(q, k, v, None, None, [L], None, 0.125)
+    X = _x(0.125, q, np.where(np.isinf(k), 0, k))
+    tol = u.HALF_STEP[dt] * (A + np.abs(ref)) + 4e-6 * X * A + (L * 2.0 ** -25 * np.abs(v).max() if dt == "f16" else 0.0)
+    assert np.all(np.abs(O - ref) <= tol), np.max(np.abs(O - ref) / tol)
+    assert np.all(np.abs(lse - ref_lse) <= 1e-6 * X + 1e-6 * (1 + np.abs(ref_lse)))
+
+
+def test_decode_huge_values_under_far_apart_scores():
+    """Values of 1e30 and a score 2^50 above the others in the middle: no accumulator overflows."""
+    L = 1000
+    x = np.zeros(L)
+    x[333] = 35.0
+    Q, K, V = _scored(x, 1, 40, 8, 2, 128, "bf16", seed=4)
+    V.mul_(1e30)
+    p = s2o.make_decode_params(1, 40, 8, 2, 128, 1, L, softmax_scale=0.125)
+    check_decode(run_decode((Q, K, V, None, None), p), Q, K, V, None, None, [L], None, "bf16", scale=0.125)
+
+
+@pytest.mark.parametrize("rows", [1, 12, 30, 70])                                    # 16, 32 and 64 rows a wavefront
+@pytest.mark.parametrize("kind", ["one far above", "rising", "falling", "first unseen", "every other unseen"])
+def test_weights_scores_far_apart(kind, rows):
+    L = 3000
+    Q, K, _ = _scored(_steps(kind, L) * (1.0 if kind != "rising" else 1.2), 1, rows, 8, 2, 128, "bf16", seed=6, gain=0.25)
+    Q = Q.abs()
+    p = s2o.make_weights_params(1, rows, 8, 2, 128, 1, L, softmax_scale=0.125)
+    w = _f(s2o.s2o_key_weights(Q, K, p))
+    with np.errstate(invalid="ignore"):
+        ref = u.key_weights(_f(Q), _f(K), [L], 0, 0.125)
+    k = _f(K)
+    tol = (2e-6 * _x(0.125, _f(Q), np.where(np.isinf(k), 0, k)) + 4e-6 + rows * 4 * 2.0 ** -25) * np.abs(ref)
+    tol += rows * 4 * 2.0 ** -126                          # exp2 gives 0 in place of a number below 2^-126: of each row's term at most that is lost
+    assert np.all(np.abs(w - ref) <= tol), np.max(np.abs(w - ref) / tol)
+
+
 def test_lengths_beyond_the_memory_are_clamped():
     t, p = make_decode(2, 2, 4, 2, 64, 1, 600, 40, "bf16")
     got = run_decode(t, p, [10 ** 9, -5], [[41, -1], [2 ** 31 - 1, 0]])
@@ -351,6 +428,37 @@ def test_evict(c):
     check_evict(e, K, V, w, lens or [L] * Z, keep, sink, recent, True)
 
 
+@pytest.mark.parametrize("L,keep,sink,recent,lens,kind", [
+    (70001, 30011, 0, 0, [70001, 65536], "equal"),         # all rows share the last one's key: more than 16384 entries
+    (70001, 40000, 4, 64, [70001, 39999], "signed"),
+    (40000, 1, 0, 0, [40000, 1], "plain"),
+    (40000, 100, 50, 50, [40000, 100], "plain"),           # nothing to choose
+    (40000, 30000, 10, 20, [0, 29999], "plain"),           # all stay
+    (40000, 30000, 10, 20, [3, 30001], "wild"),
+    (32769, 16000, 4096, 4096, [32769, 32768], "ties"),
+])
+def test_evict_long(L, keep, sink, recent, lens, kind):
+    g = _gen(L + keep)
+    K, V = (u.randn(g, 2, 2, L, 64) for _ in range(2))
+    w = _weights(g, 2, 2, L, kind)
+    p = s2o.make_evict_params(2, 2, 64, L, keep, sink, recent)
+    e = s2o.s2o_evict(K, V, w, p, lens=_i32(lens))
+    torch.cuda.synchronize()
+    check_evict(e, K, V, w, lens, keep, sink, recent, False)
+
+
+def test_evict_selects_among_nine_million():
+    """Stretches of more than one block of rows."""
+    g = _gen(8)
+    L, keep = 9_000_001, 5000
+    w = torch.rand(1, 1, L, generator=g).cuda()
+    w[0, 0, ::1000] = 2.0                                  # 9001 rows share the highest weight
+    e = s2o.s2o_evict(None, None, w, s2o.make_evict_params(1, 1, 64, L, keep, 3, 5))
+    at = np.concatenate([[0, 1, 2], np.arange(1, keep - 7) * 1000, np.arange(L - 5, L)])
+    assert at.size == keep and int(e.lens[0]) == keep and np.array_equal(e.kept[0, 0].cpu().numpy(), at)
+    assert torch.equal(e.weights[0, 0], w[0, 0, torch.from_numpy(at).cuda()])
+
+
 def test_evict_moves_bits_and_allocates():
     """Rows are moved, not read as numbers: NaNs keep their payload.  Outputs that are not given are allocated."""
     g = _gen(2)
@@ -427,6 +535,22 @@ def test_another_stream():
     w = s2o.s2o_key_weights(t[0], t[1], s2o.make_weights_params(1, 3, 4, 2, 64, 1, 2000, dtype="f16"), lse=b[1], lens=_i32([1999]), stream=s)
     s.synchronize()
     assert _same(a, b) and (w[..., 1999:] == 0).all()
+
+
+def test_two_streams_at_once():
+    """Calls with buffers and workspaces of their own, on two streams together."""
+    sides = [_three(seed) for seed in (3, 4)]
+    for run, _, _ in sides:
+        run()
+    torch.cuda.synchronize()
+    first = [[x.clone() for x in outs] for _, outs, _ in sides]
+    streams = [torch.cuda.Stream() for _ in sides]
+    for _ in range(5):
+        for (run, _, _), s in zip(sides, streams):
+            run(stream=s)
+    torch.cuda.synchronize()
+    for (_, outs, _), want in zip(sides, first):
+        assert _same(outs, want)
 
 
 def test_captured_and_replayed():
