@@ -198,14 +198,14 @@ def _keep_alive_on(stream, *tensors):
             t.record_stream(stream)
 
 
-def _stream_handle(stream) -> Optional[int]:
+def _stream_handle(stream, current_device=None) -> Optional[int]:
     import torch
     if stream is None:
         # torch's own entry leaves out the Stream object around the handle (0.3 instead of 2.9 us a call); it is not
         # a public one and need not be there
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is not None:
-            return raw(torch.cuda.current_device()) or None
+            return raw(torch.cuda.current_device() if current_device is None else current_device) or None
         stream = torch.cuda.current_stream()
     return stream.cuda_stream or None
 
@@ -472,8 +472,9 @@ def _on_device(dev, stream):
     import torch
     if stream is not None and getattr(stream, "device", dev) != dev:
         raise ValueError(f"stream: on {stream.device}, the tensors on {dev}")
-    if dev.index == torch.cuda.current_device():
-        return _stream_handle(stream), None
+    current = torch.cuda.current_device()
+    if dev.index == current:
+        return _stream_handle(stream, current), None
     if stream is None:
         stream = torch.cuda.current_stream(dev)
     return stream.cuda_stream or None, torch.cuda.device(dev)
@@ -516,7 +517,9 @@ def s2o_decode(Q, K, V, params: S2ODecodeParams, own_K=None, own_V=None, lens=No
     fresh = []
     if O is None:
         shape, strides = layout["O"]
-        if strides is None:
+        if strides is None and layout["Q"][1] is None:
+            O = torch.empty_like(Q)                      # (packed like it; quicker)
+        elif strides is None:
             O = torch.empty(shape, dtype=dtype, device=dev)
         else:
             O = torch.empty_strided(shape, strides + (1,), dtype=dtype, device=dev)
