@@ -4,9 +4,9 @@
 // Weights are ranked by an unsigned key that orders like the float (-0 as +0, NaN as -inf).  What stays is the rows above the key of the
 // last one, and of those that share it the first few.
 //   select_kernel  up to 32K rows, a workgroup per (cache, KV head): all keys, and counts of 11, 11 and 10 of their bits, in LDS
-//   count_kernel, collect_kernel, list_kernel    more rows, a workgroup per stretch of 4096: count the keys' upper 11 bits; collect the
-//                  other 21 bits of the rows that share the last one's; settle them (every workgroup for itself, from LDS where they
-//                  fit) and list.  Three passes over the weights by all of the chip: one workgroup a head took 102 us
+//   count_kernel, collect_kernel, list_kernel    more rows, a workgroup per stretch of 4096 or more: count the keys' upper 11 bits; collect
+//                  the other 21 bits of the rows that share the last one's; settle them (every workgroup for itself, from LDS where they
+//                  fit) and list.  Nothing is added up by atomics in memory, so that nothing has to be cleared.  Three passes over the weights by all of the chip: one workgroup a head took 102 us
 //                  for 8 heads of 128K rows, bound by the instructions of one CU.
 // gather_kernel copies the listed rows of K and V and their weights.  Bound: HBM bandwidth of the copy.
 #include "cache_tile.h"
@@ -41,7 +41,8 @@ struct Places {
 constexpr int kT = 1024, kWaves = kT / 64;
 constexpr int kOneGroup = 32 * kT;  // rows that select_kernel takes
 constexpr int kBlock = 4 * kT;      // rows that a workgroup looks at at once, four in a row a thread
-constexpr int kStretches = 2048;    // of a row of weights at most: a stretch's number takes the 11 bits that an entry's key leaves
+constexpr int kStretches = 64;      // a head's rows are cut into, as far as a stretch has no more than kMostBlocks blocks
+constexpr int kMostBlocks = 15;     // (its counts have 16 bits)
 constexpr int kBins = 2048;
 constexpr int kRoom = 16384;        // entries that list_kernel keeps in LDS
 
@@ -75,37 +76,46 @@ __device__ __forceinline__ Sums block_scan(int a, int b, int2* part, int tid) {
   return s;
 }
 
-// counts[0 .. kBins - 1] -> the bin of the want-th largest (1 <= want <= the counts' sum), how many it holds, and how many lie in larger bins.
-struct Bin { int bin, holds, above; };
-__device__ __forceinline__ Bin find_bin(const uint32_t* counts, int2* part, Bin* found, int want, int tid) {
+// The bin of the want-th largest (1 <= want <= the counts' sum), how many it holds, and how many lie in larger bins.  Bins are dealt out from
+// the largest down, two a thread: c, with `tag` to be had back of the bin that is found.
+constexpr int bins_of(int tid) { return kBins - 2 - 2 * tid; }
+struct Bin { int bin, holds, above, tag; };
+__device__ __forceinline__ Bin find_bin(uint2 c, uint2 tag, int2* part, Bin* found, int want, int tid) {
   static_assert(kBins == 2 * kT, "two bins a thread");
-  const int b = kBins - 2 - 2 * tid;                       // the largest first
-  const uint2 c = *reinterpret_cast<const uint2*>(counts + b);
+  const int b = bins_of(tid);
   const int own = (int)(c.x + c.y), before = block_scan(own, 0, part, tid).a;
   if (before < want && before + own >= want) {
     const bool upper = before + (int)c.y >= want;
-    *found = upper ? Bin{b + 1, (int)c.y, before} : Bin{b, (int)c.x, before + (int)c.y};
+    *found = upper ? Bin{b + 1, (int)c.y, before, (int)tag.y} : Bin{b, (int)c.x, before + (int)c.y, (int)tag.x};
   }
   __syncthreads();
   return *found;
 }
+__device__ __forceinline__ Bin find_bin(const uint32_t* counts, int2* part, Bin* found, int want, int tid) {
+  return find_bin(*reinterpret_cast<const uint2*>(counts + bins_of(tid)), uint2{0, 0}, part, found, want, tid);
+}
 
-__host__ __device__ inline int stretch_rows(int L) { return (int)(((int64_t)L + (int64_t)kStretches * kBlock - 1) / ((int64_t)kStretches * kBlock)) * kBlock; }
+__host__ __device__ inline int stretch_rows(int L) {
+  const int64_t blocks = ((int64_t)L + (int64_t)kStretches * kBlock - 1) / ((int64_t)kStretches * kBlock);
+  return kBlock * (int)(blocks < kMostBlocks ? blocks : kMostBlocks);
+}
 __host__ __device__ inline int stretches(int L) { return (L + stretch_rows(L) - 1) / stretch_rows(L); }
 
-// The scratch words of a head: counts, then what the kernels hand on, then entries.
+// The scratch words of a head: counts of its stretches, then what the kernels hand on, then entries.
 struct Scratch {
-  uint32_t* counts;    // [kBins] of the keys' upper 11 bits
-  uint32_t* known;     // [0]: those of the last row that stays, [1]: places for the rows that share them, [2]: entries
+  uint32_t* counts;    // [stretches][kBins / 2]: pairs of counts of the keys' upper 11 bits
+  uint32_t* known;     // [0]: those of the last row that stays, [1]: places for the rows that share them, [2]: how many do
   uint32_t* above;     // [stretches] rows of larger upper bits
-  uint32_t* entries;   // rows that share them: the other 21 bits, and the stretch
-  static constexpr int kHead = kBins + 64;
-  static __host__ __device__ size_t words(int L) { return kHead + (size_t)(stretches(L) + 63) / 64 * 64 + ((size_t)L + 63) / 64 * 64; }
+  uint32_t* first;     // [stretches] rows in front of the stretch that share them
+  uint32_t* entries;   // the other 21 bits of those that do, stretch after stretch
+  static __host__ __device__ size_t list_words(int L) { return (size_t)(stretches(L) + 63) / 64 * 64; }
+  static __host__ __device__ size_t words(int L) { return (size_t)stretches(L) * (kBins / 2) + 64 + 2 * list_words(L) + ((size_t)L + 63) / 64 * 64; }
   __device__ __forceinline__ Scratch(const EvictArgs& a, int64_t head) {
     counts = a.scratch + head * (int64_t)words(a.L);
-    known = counts + kBins;
-    above = counts + kHead;
-    entries = above + (stretches(a.L) + 63) / 64 * 64;
+    known = counts + (size_t)stretches(a.L) * (kBins / 2);
+    above = known + 64;
+    first = above + list_words(a.L);
+    entries = first + list_words(a.L);
   }
 };
 
@@ -129,12 +139,6 @@ __device__ __forceinline__ void list_rows(int32_t* list, int from, uint64_t sure
   }
 }
 
-__global__ __launch_bounds__(256) void clear_kernel(const EvictArgs a) {
-  touch_args<EvictArgs>();
-  const Scratch s(a, blockIdx.x);
-  for (int i = threadIdx.x; i < Scratch::kHead; i += 256) s.counts[i] = 0;
-}
-
 __global__ __launch_bounds__(kT) void count_kernel(const EvictArgs a) {
   touch_args<EvictArgs>();
   __shared__ uint32_t counts[kBins];
@@ -155,16 +159,14 @@ __global__ __launch_bounds__(kT) void count_kernel(const EvictArgs a) {
       if (i + e >= p.lo && i + e < to) atomicAdd(&counts[k[e] >> 21], 1u);
   }
   __syncthreads();
-  const Scratch s(a, head);
-  for (int i = tid; i < kBins; i += kT)
-    if (counts[i]) atomicAdd(&s.counts[i], counts[i]);
+  const uint2 c = *reinterpret_cast<const uint2*>(counts + 2 * tid);
+  Scratch(a, head).counts[(int64_t)stretch * (kBins / 2) + tid] = c.x | c.y << 16;
 }
 
 __global__ __launch_bounds__(kT) void collect_kernel(const EvictArgs a) {
   touch_args<EvictArgs>();
   __shared__ int2 part[kWaves];
   __shared__ Bin found;
-  __shared__ uint32_t base;
   const int tid = threadIdx.x;
   const int stretch = (int)(blockIdx.x % stretches(a.L));
   const int64_t head = blockIdx.x / stretches(a.L);
@@ -172,17 +174,32 @@ __global__ __launch_bounds__(kT) void collect_kernel(const EvictArgs a) {
   const int per = stretch_rows(a.L), from = stretch * per, to = min(p.hi, from + per);
   if (!p.choose() || from >= p.n) return;
   const Scratch s(a, head);
-  const Bin last = find_bin(s.counts, part, &found, p.want, tid);
+  const float* w = a.weights + head * a.L;
+  uint32_t next[4];                                        // keys of the first block, on their way meanwhile
+  four(w, from + 4 * tid, p.n, next);
+  uint2 all = {0, 0}, front = {0, 0};                      // counts of all stretches, and of those in front
+  const int counted = (p.hi + per - 1) / per;
+#pragma unroll 16
+  for (int i = 0; i < counted; ++i) {
+    const uint32_t c = s.counts[(int64_t)i * (kBins / 2) + bins_of(tid) / 2];
+    all.x += c & 0xffffu;
+    all.y += c >> 16;
+    front.x += i < stretch ? c & 0xffffu : 0u;
+    front.y += i < stretch ? c >> 16 : 0u;
+  }
+  const Bin last = find_bin(all, front, part, &found, p.want, tid);
   if (stretch == 0 && tid == 0) {
     s.known[0] = (uint32_t)last.bin;
     s.known[1] = (uint32_t)(p.want - last.above);
+    s.known[2] = (uint32_t)last.holds;
   }
-  const float* w = a.weights + head * a.L;
-  int above = 0;
+  int above = 0, base = last.tag;
   for (int i0 = from; i0 < to; i0 += kBlock) {
     const int i = i0 + 4 * tid;
     uint32_t k[4];
-    four(w, i, p.n, k);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) k[e] = next[e];
+    if (i0 + kBlock < to) four(w, i + kBlock, p.n, next);
     int mine = 0, larger = 0;
     bool same[4];
 #pragma unroll
@@ -192,17 +209,18 @@ __global__ __launch_bounds__(kT) void collect_kernel(const EvictArgs a) {
       same[e] = in && (int)(k[e] >> 21) == last.bin;
       mine += same[e];
     }
-    // room for them.  (Entries are a set: their order does not matter.)
     const Sums sums = block_scan(mine, larger, part, tid);
     above += sums.all_b;
-    if (tid == 0) base = sums.all_a ? atomicAdd(&s.known[2], (uint32_t)sums.all_a) : 0u;
-    __syncthreads();
-    int at = (int)base + sums.a;
+    int at = base + sums.a;
+    base += sums.all_a;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (same[e]) s.entries[at++] = (k[e] & 0x1fffffu) | (uint32_t)stretch << 21;
+      if (same[e]) s.entries[at++] = k[e] & 0x1fffffu;
   }
-  if (tid == 0) s.above[stretch] = (uint32_t)above;
+  if (tid == 0) {
+    s.above[stretch] = (uint32_t)above;
+    s.first[stretch] = (uint32_t)last.tag;
+  }
 }
 
 __global__ __launch_bounds__(kT) void list_kernel(const EvictArgs a) {
@@ -219,10 +237,13 @@ __global__ __launch_bounds__(kT) void list_kernel(const EvictArgs a) {
   if (from >= to) return;
   const Scratch s(a, head);
   const bool choose = p.choose(), all = !choose && p.want > 0;
+  const float* w = a.weights + head * a.L;
+  uint32_t next[4];
+  four(w, from + 4 * tid, p.n, next);
   uint32_t key = 0;
   int ties = 0, kept_before = all ? from : min(p.lo, from) + max(0, from - p.hi), tied_before = 0;
   if (choose) {
-    const int used = (int)s.known[2], here = min(used, kRoom);
+    const int used = (int)s.known[2], here = min(used, kRoom), first = (int)s.first[stretch];
     key = s.known[0] << 21;
     ties = (int)s.known[1];
     int kept = 0, tied = 0;
@@ -231,9 +252,9 @@ __global__ __launch_bounds__(kT) void list_kernel(const EvictArgs a) {
     for (int i = tid; i < here; i += kT) room[i] = s.entries[i];
     auto each = [&](auto f) {
 #pragma unroll 1
-      for (int i = tid; i < here; i += kT) f(room[i]);
+      for (int i = tid; i < here; i += kT) f(room[i], i);
 #pragma unroll 1
-      for (int i = kRoom + tid; i < used; i += kT) f(s.entries[i]);
+      for (int i = kRoom + tid; i < used; i += kT) f(s.entries[i], i);
     };
     // 11 and 10 bits more
 #pragma unroll 1
@@ -242,8 +263,7 @@ __global__ __launch_bounds__(kT) void list_kernel(const EvictArgs a) {
       __syncthreads();
       for (int i = tid; i < kBins; i += kT) counts[i] = 0;
       __syncthreads();
-      each([&](uint32_t x) {
-        const uint32_t k = x & 0x1fffffu;
+      each([&](uint32_t k, int) {
         if ((k >> known) == ((key & 0x1fffffu) >> known)) atomicAdd(&counts[(k >> shift) & mask], 1u);
       });
       __syncthreads();
@@ -252,21 +272,21 @@ __global__ __launch_bounds__(kT) void list_kernel(const EvictArgs a) {
       ties -= last.above;
     }
     // what stays in front of this stretch, for certain and if there are places
-    each([&](uint32_t x) {
-      const uint32_t k = x & 0x1fffffu, last = key & 0x1fffffu;
-      const bool front = (int)(x >> 21) < stretch;
-      kept += front && k > last;
-      tied += front && k == last;
+    each([&](uint32_t k, int i) {
+      const uint32_t last = key & 0x1fffffu;
+      kept += i < first && k > last;
+      tied += i < first && k == last;
     });
     const Sums sums = block_scan(kept, tied, part, tid);
     kept_before += sums.all_a;
     tied_before = sums.all_b;
   }
-  const float* w = a.weights + head * a.L;
   for (int i0 = from; i0 < to; i0 += kBlock) {
     const int i = i0 + 4 * tid;
     uint32_t k[4], sure = 0, tie = 0;
-    four(w, i, p.n, k);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) k[e] = next[e];
+    if (i0 + kBlock < to) four(w, i + kBlock, p.n, next);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const bool competes = i + e >= p.lo && i + e < p.hi;
@@ -408,7 +428,6 @@ hipError_t launch_evict(EvictArgs a, void* scratch, hipStream_t stream) {
     const int64_t blocks = heads * stretches(a.L);
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks);
-    hipLaunchKernelGGL(clear_kernel, dim3((unsigned)heads), dim3(256), 0, stream, a);
     hipLaunchKernelGGL(count_kernel, grid, dim3(kT), 0, stream, a);
     hipLaunchKernelGGL(collect_kernel, grid, dim3(kT), 0, stream, a);
     hipLaunchKernelGGL(list_kernel, grid, dim3(kT), 0, stream, a);
