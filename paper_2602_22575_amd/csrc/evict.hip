@@ -3,7 +3,7 @@
 //
 // Weights are ranked by an unsigned key that orders like the float (-0 as +0, NaN as -inf).  What stays is the rows above the key of the
 // last one, and of those that share it the first few.
-//   select_kernel  up to 32K rows, a workgroup per (cache, KV head): all keys, and counts of 11, 11 and 10 of their bits, in LDS
+//   select_kernel  up to 20K rows, a workgroup per (cache, KV head): all keys, and counts of 11, 11 and 10 of their bits, in LDS
 //   count_kernel, collect_kernel, list_kernel    more rows, a workgroup per stretch of 4096 or more: count the keys' upper 11 bits; collect
 //                  the other 21 bits of the rows that share the last one's; settle them (every workgroup for itself, from LDS where they
 //                  fit) and list.  Nothing is added up by atomics in memory, so that nothing has to be cleared.  Three passes over the weights by all of the chip: one workgroup a head took 102 us
@@ -39,7 +39,7 @@ struct Places {
 };
 
 constexpr int kT = 1024, kWaves = kT / 64;
-constexpr int kOneGroup = 32 * kT;  // rows that select_kernel takes
+constexpr int kOneGroup = 20 * kT;  // rows that select_kernel takes (8 heads of 16K rows 25 us, of 32K 42; by stretches 26 and 33)
 constexpr int kBlock = 4 * kT;      // rows that a workgroup looks at at once, four in a row a thread
 constexpr int kStretches = 64;      // a head's rows are cut into, as far as a stretch has no more than kMostBlocks blocks
 constexpr int kMostBlocks = 15;     // (its counts have 16 bits)
@@ -119,11 +119,12 @@ struct Scratch {
   }
 };
 
-// Keys of four rows from row i on (behind the end: the last row's).  n > 0.  (Four loads without a branch rather than one with: several
-// calls' are in flight together.)
+// Keys of four rows i, i + step, .. (behind the end: the last row's).  n > 0.  (Four loads without a branch rather than one with: several
+// calls' are in flight together.)  Steps of 1 only where a thread needs rows in a row: it reads sixteen lines an instruction, not four.
+template <int kStep>
 __device__ __forceinline__ void four(const float* w, int i, int n, uint32_t (&k)[4]) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) k[e] = rank_key(w[min(i + e, n - 1)]);
+  for (int e = 0; e < 4; ++e) k[e] = rank_key(w[min(i + kStep * e, n - 1)]);
 }
 
 // Lists rows of a thread: from + j for the bits j of `sure`, and of `tie` those that find a place.  s, t: such rows in front of the thread's.
@@ -151,12 +152,12 @@ __global__ __launch_bounds__(kT) void count_kernel(const EvictArgs a) {
   for (int i = tid; i < kBins; i += kT) counts[i] = 0;
   __syncthreads();
   const float* w = a.weights + head * a.L;
-  for (int i = from + 4 * tid; i < to; i += kBlock) {
+  for (int i = from + tid; i < to; i += kBlock) {
     uint32_t k[4];
-    four(w, i, p.n, k);
+    four<kT>(w, i, p.n, k);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (i + e >= p.lo && i + e < to) atomicAdd(&counts[k[e] >> 21], 1u);
+      if (i + kT * e >= p.lo && i + kT * e < to) atomicAdd(&counts[k[e] >> 21], 1u);
   }
   __syncthreads();
   const uint2 c = *reinterpret_cast<const uint2*>(counts + 2 * tid);
@@ -176,7 +177,7 @@ __global__ __launch_bounds__(kT) void collect_kernel(const EvictArgs a) {
   const Scratch s(a, head);
   const float* w = a.weights + head * a.L;
   uint32_t next[4];                                        // keys of the first block, on their way meanwhile
-  four(w, from + 4 * tid, p.n, next);
+  four<kT>(w, from + tid, p.n, next);
   uint2 all = {0, 0}, front = {0, 0};                      // counts of all stretches, and of those in front
   const int counted = (p.hi + per - 1) / per;
 #pragma unroll 16
@@ -195,16 +196,16 @@ __global__ __launch_bounds__(kT) void collect_kernel(const EvictArgs a) {
   }
   int above = 0, base = last.tag;
   for (int i0 = from; i0 < to; i0 += kBlock) {
-    const int i = i0 + 4 * tid;
+    const int i = i0 + tid;
     uint32_t k[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) k[e] = next[e];
-    if (i0 + kBlock < to) four(w, i + kBlock, p.n, next);
+    if (i0 + kBlock < to) four<kT>(w, i + kBlock, p.n, next);
     int mine = 0, larger = 0;
     bool same[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const bool in = i + e >= p.lo && i + e < to;
+      const bool in = i + kT * e >= p.lo && i + kT * e < to;
       larger += in && (int)(k[e] >> 21) > last.bin;
       same[e] = in && (int)(k[e] >> 21) == last.bin;
       mine += same[e];
@@ -239,7 +240,7 @@ __global__ __launch_bounds__(kT) void list_kernel(const EvictArgs a) {
   const bool choose = p.choose(), all = !choose && p.want > 0;
   const float* w = a.weights + head * a.L;
   uint32_t next[4];
-  four(w, from + 4 * tid, p.n, next);
+  four<1>(w, from + 4 * tid, p.n, next);
   uint32_t key = 0;
   int ties = 0, kept_before = all ? from : min(p.lo, from) + max(0, from - p.hi), tied_before = 0;
   if (choose) {
@@ -286,7 +287,7 @@ __global__ __launch_bounds__(kT) void list_kernel(const EvictArgs a) {
     uint32_t k[4], sure = 0, tie = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) k[e] = next[e];
-    if (i0 + kBlock < to) four(w, i + kBlock, p.n, next);
+    if (i0 + kBlock < to) four<1>(w, i + kBlock, p.n, next);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const bool competes = i + e >= p.lo && i + e < p.hi;
@@ -317,16 +318,20 @@ __global__ __launch_bounds__(kT) void select_kernel(const EvictArgs a) {
   const bool choose = p.choose(), all = !choose && p.want > 0;
   for (int i = tid; i < kBins; i += kT) counts[i] = 0;
   __syncthreads();
-#pragma unroll 4
-  for (int i = 4 * tid; i < p.n; i += kBlock) {
-    uint32_t k[4];
-    four(w, i, p.n, k);
+  constexpr int kFours = 2;                                // in flight together
+  for (int i = tid; i < p.n; i += kFours * kBlock) {
+    uint32_t k[kFours][4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (i + e < p.lo || i + e >= p.hi) k[e] = 0;
-      if (k[e] && choose) atomicAdd(&counts[k[e] >> 21], 1u);
-    }
-    *reinterpret_cast<u32x4*>(keys + i) = u32x4{k[0], k[1], k[2], k[3]};
+    for (int j = 0; j < kFours; ++j) four<kT>(w, i + j * kBlock, p.n, k[j]);
+#pragma unroll
+    for (int j = 0; j < kFours; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int at = i + j * kBlock + kT * e;
+        if (at < p.lo || at >= p.hi) k[j][e] = 0;
+        if (k[j][e] && choose) atomicAdd(&counts[k[j][e] >> 21], 1u);
+        if (at < p.n) keys[at] = k[j][e];
+      }
   }
   __syncthreads();
   // From here on a thread has a stretch of its own: an odd number of pieces of four rows, so that a wavefront's reads meet different banks.
