@@ -16,7 +16,12 @@
 // private 32 x D of LDS for the transposing read.  The next tile's loads are issued as soon as the score products have consumed the
 // current ones.  Bound: HBM bandwidth.
 // Blocks of 128 rows share tiles of 64 keys between four wavefronts of 32 rows each (Walk::wide): global memory goes
-// straight to LDS, one tile ahead.  Bound: HBM bandwidth up to about 256 rows a KV head, the matrix cores beyond.
+// straight to LDS, one tile ahead (one and a half ahead, with a second barrier a tile, was 2 to 4 % slower).  Bound: HBM bandwidth up to
+// about 256 rows a KV head, the matrix cores beyond.
+//
+// Measured, bf16, D 128, 32 query heads on 8: one sequence on 32K keys 26 us and 4 for the join, 5.2 TB/s; 32 sequences on 32K keys and up to
+// 512 of their own each 42 and 7; 64 on 128K and up to 1024 of their own 163 and 8, 0.77 PFLOP/s.  Of a launch 3 us pass until
+// the first keys are asked for (arguments, indices, the first pass through the code) and 3 while the parts' states are written.
 #include <type_traits>
 
 #include "cache_tile.h"
@@ -233,7 +238,7 @@ struct Walk {
   //
   // The first 16 keys find the references, the last tiles may have hidden keys.  For the others, if `fast`, a tile's products and exponentials
   // are one straight run of instructions, its second half's exponentials behind its first half's products: numerators are formed
-  // against the references as they are, and a reference moves afterwards, where a tile's sum has outgrown 2^10.  Returns false where a numerator
+  // against the references as they are, and a reference moves afterwards, where two tiles' sum has outgrown 2^10.  Returns false where a numerator
   // or an accumulator may have outgrown its type on the way: all of it is to be done again, not fast.
   template <class F>
   __device__ __forceinline__ bool wide(const E* K, const E* V, int64_t kstride, int64_t vstride, int len, int from, int to, float c2,
@@ -290,7 +295,7 @@ struct Walk {
       meet();
     };
     bool fits = true;
-    auto fast_tile = [&](int t, unsigned char* kt, unsigned char* vt, unsigned char* knext, unsigned char* vnext) {
+    auto fast_tile = [&](int t, unsigned char* kt, unsigned char* vt, unsigned char* knext, unsigned char* vnext, float (&sum)[CB]) {
       if (t + 1 < to) fetch(t + 1, knext, vnext);
       // K operands in pairs p = (32-key half, 32 dims), two pairs ahead of their products; V operands behind them, four ahead.  Every
       // product, and what stands behind it, is a scheduling region of its own.
@@ -299,7 +304,7 @@ struct Walk {
       static_assert(CB == 2 && kEach * 2 * kDims * CB == 16 && kBlocks == 2 * kDims);
       f32x4 s[4][CB];
       x8 kf[kPairs][2], vf[2 * kBlocks], pb[2][CB];
-      float sum[CB] = {}, p[2][16];
+      float p[2][16];
       auto read_keys = [&](int pair) {
 #pragma unroll
         for (int e = 0; e < 2; ++e)
@@ -355,28 +360,32 @@ struct Walk {
           __builtin_amdgcn_sched_barrier(0);
         }
       }
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) asm volatile("" : "+v"(sum[cb]));      // (added up where the numerators are made)
+      meet();
+    };
+    // Behind a run of fast tiles with these sums: references that have to move do.
+    auto settle = [&](const float (&sum)[CB]) {
       bool moves = false;
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
         l[cb] += sum[cb];
         moves |= !(sum[cb] <= kMove);
       }
-      if (__builtin_amdgcn_ballot_w64(moves) != 0) {
+      if (__builtin_amdgcn_ballot_w64(moves) == 0) return;
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-          const float most = column_max(sum[cb]);
-          fits &= !(__builtin_amdgcn_ballot_w64(!(sum[cb] <= kMost)) != 0);
-          const int up = most > kMove && most <= kMost ? __builtin_amdgcn_frexp_expf(most) : 0;
-          const float alpha = __builtin_amdgcn_ldexpf(1.0f, -up);
-          m[cb] += (float)up;
-          l[cb] *= alpha;
+      for (int cb = 0; cb < CB; ++cb) {
+        const float most = column_max(sum[cb]);
+        fits &= !(__builtin_amdgcn_ballot_w64(!(sum[cb] <= kMost)) != 0);
+        const int up = most > kMove && most <= kMost ? __builtin_amdgcn_frexp_expf(most) : 0;
+        const float alpha = __builtin_amdgcn_ldexpf(1.0f, -up);
+        m[cb] += (float)up;
+        l[cb] *= alpha;
 #pragma unroll
-          for (int db = 0; db < D / 16; ++db)
+        for (int db = 0; db < D / 16; ++db)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[cb][db][i] *= alpha;
-        }
+          for (int i = 0; i < 4; ++i) o[cb][db][i] *= alpha;
       }
-      meet();
     };
     fetch(from, ka, va);
     rows(lim, lim_all);
@@ -395,9 +404,16 @@ struct Walk {
         fits &= __builtin_amdgcn_ballot_w64(!(fabsf(first) < INFINITY)) == 0;
       }
     }
-    for (; t < full; t += 2) {
-      fast_tile(t, ka, va, kb_, vb);
-      if (t + 1 < full) fast_tile(t + 1, kb_, vb, ka, va);
+    for (; t + 1 < full; t += 2) {                         // (one place for moving: two made the compiler copy all accumulators once a tile)
+      float sum[CB] = {};
+      fast_tile(t, ka, va, kb_, vb, sum);
+      fast_tile(t + 1, kb_, vb, ka, va, sum);
+      settle(sum);
+    }
+    if (t < full) {
+      float sum[CB] = {};
+      fast_tile(t, ka, va, kb_, vb, sum);
+      settle(sum);
     }
     for (t = max(from, full); t < to; ++t) {
       const bool odd = (t - from) & 1;

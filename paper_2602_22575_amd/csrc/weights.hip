@@ -11,6 +11,10 @@
 //                  atomics, the same bits every time.
 // Rows are counted r = (t * B + b) * G + g, so that what a key is seen by is one range of rows.
 //
+// Bound: a score costs 2 D FLOP on the matrix cores and an exponential, a multiply-add and an addition on the vector units, which take about as
+// long; the two overlap by half.  64 queries of 32 heads on 128K keys of 8 (69 GFLOP a pass): statistics 79 us, sums 86, 0.87 and 0.80
+// PFLOP/s; in the first the matrix cores work 43 % of the time, the vector units 63 %, one or the other 89 %.
+//
 // Statistics are kept as a base-2 reference m and 1/l instead of one lse: rounding m + log2 l would cost the weights
 // 2^-20 of their value.  An lse that is given is turned into the same pair, its base-2 form rounded and the rest in the factor.
 #include "cache_tile.h"
@@ -69,8 +73,7 @@ __device__ __forceinline__ void order_tile() {
 }
 
 // Streams tiles from .. to - 1 of 64 keys through three LDS buffers, two tiles ahead of the one that is worked on: two workgroups a CU
-// then have 64 KB on their way (with one tile ahead the kernels waited for memory).  All threads of
-// the workgroup; fast(t, tile) or, where it returns false, any(t, tile) works on tile t; the buffers are separate arrays, so
+// then have 64 KB on their way (with one tile ahead the kernels waited for memory).  All threads of the workgroup; fast(t, tile) or, where it returns false, any(t, tile) works on tile t; the buffers are separate arrays, so
 // that the compiler sees that reads of one need not wait for the loads that fill another.
 template <class E, int D, class F, class G>
 __device__ __forceinline__ void stream_keys(const E* K, int64_t stride, int len, int from, int to, unsigned char* b0, unsigned char* b1,
