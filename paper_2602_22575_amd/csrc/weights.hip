@@ -54,22 +54,38 @@ __device__ __forceinline__ void share(const Divisor& by_parts, int all, int part
 // Keys that query token t sees.
 __device__ __forceinline__ int row_limit(const WeightsArgs& a, int len, int t) { return a.causal ? min(max(len - a.T + t + 1, 0), len) : len; }
 
-// The order of a tile's instructions: the products of a block of 16 keys one by one, behind each its share of the three instructions a score that the
-// block before it takes.  (Left to itself the compiler waits for one block's results and then works on them.)
-template <int D, int CB>
-__device__ __forceinline__ void order_tile() {
-  constexpr int kReads = D / 32, kProducts = CB * kReads, kVector = 12 / kReads;
-  __builtin_amdgcn_sched_group_barrier(0x100, 2 * kReads, 0);      // LDS reads
-  __builtin_amdgcn_sched_group_barrier(0x8, kProducts, 0);         // MFMA
+// A tile of 64 keys in this order of instructions: the products of a block of 16 keys one by one, behind each its share of the values (scores)
+// of the block before; keys are read a block ahead.  Every product, and what stands behind it, is a scheduling region of its
+// own.  (Left to itself the compiler waits for one block's results and then works on them.)  product(k, kk, cb, s): s plus the product of 32
+// dims; value(kb, x, s): works on score 4 * column block + i of 4 * CB in a lane.
+template <class E, int D, int CB, class P, class V>
+__device__ __forceinline__ void tile_in_order(const unsigned char* tile, int mm, int g, P product, V value) {
+  typedef typename Vec<E>::x8 x8;
+  constexpr int kReads = D / 32, kEach = 4 / kReads;
+  x8 k[2][kReads];
+  f32x4 s[2][CB];
+  auto read = [&](int kb, int kk) { k[kb & 1][kk] = *reinterpret_cast<const x8*>(tile + 16 * kb * 2 * D + (at<D>(mm, g) ^ (kk << 6))); };
 #pragma unroll
-  for (int kb = 0; kb < 3; ++kb)
+  for (int kk = 0; kk < kReads; ++kk) read(0, kk);
 #pragma unroll
-    for (int j = 0; j < kProducts; ++j) {
-      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x402, kVector, 0);     // VALU, transcendental
-      if (kb < 2 && j % CB == CB - 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+    for (int kk = 0; kk < kReads; ++kk) {
+      if (kb < 3) read(kb + 1, kk);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        f32x4& x = s[kb & 1][cb];
+        x = product(k[kb & 1][kk], kk, cb, kk == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : x);
+        if (kb > 0) {
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) value(kb - 1, (kk * CB + cb) * kEach + e, s[(kb - 1) & 1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
-  __builtin_amdgcn_sched_group_barrier(0x402, 12 * CB, 0);
+#pragma unroll
+  for (int x = 0; x < 4 * CB; ++x) value(3, x, s[1]);
 }
 
 // Streams tiles from .. to - 1 of 64 keys through three LDS buffers, two tiles ahead of the one that is worked on: two workgroups a CU
@@ -137,20 +153,17 @@ struct Stats {
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) s[cb] = mfma(k[kk], q[cb][kk], s[cb]);
   }
-  // All 64 keys seen, against the references as they are.  Exponentials of a block of 16 keys stand behind the products of the next one.
+  // All 64 keys seen, against the references as they are.
   __device__ __forceinline__ bool tile_fast(const unsigned char* tile, float c2, int mm, int g) {
-    f32x4 s[2][CB];
-    float sum[CB] = {};
-    scores(tile, 0, s[0], mm, g);
-#pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
-      if (kb < 3) scores(tile, kb + 1, s[(kb + 1) & 1], mm, g);
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[cb] += exp2_(fmaf(s[kb & 1][cb][i], c2, -m[cb]));
-    }
-    order_tile<D, CB>();
+    float sum[CB] = {}, last = 0.f;                // a numerator is added behind the next one's exponential, which it would wait for
+    tile_in_order<E, D, CB>(
+        tile, mm, g, [&](const x8& k, int kk, int cb, const f32x4& s) { return mfma(k, q[cb][kk], s); },
+        [&](int, int x, const f32x4 (&s)[CB]) {
+          const float p = exp2_(fmaf(s[x >> 2][x & 3], c2, -m[x >> 2]));
+          sum[(x + 4 * CB - 1) / 4 % CB] += last;  // (of the value before this one)
+          last = p;
+        });
+    sum[CB - 1] += last;
     bool fits = true;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) fits &= l[cb] + sum[cb] <= kRoomAbove;    // (false for NaN)
@@ -388,18 +401,17 @@ __global__ __launch_bounds__(kThreads, 2) void sum_kernel(const WeightsArgs) {
           if (active) {
             // some row does not see all of the keys, or is none
             if (__builtin_amdgcn_ballot_w64(lane < 16 * CB && my_lim < (t + 1) * kTileRows) != 0) return false;
-            // exponentials of a block of 16 keys stand behind the products of the next one
-            f32x4 s[2][CB];
-            scores(tile, 0, s[0]);
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb) {
-              if (kb < 3) scores(tile, kb + 1, s[(kb + 1) & 1]);
-#pragma unroll
-              for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sum[kb] = fmaf(exp2_(fmaf(s[kb & 1][cb][i], a.c2, -ref[cb][i])), inv[cb][i], sum[kb]);
-            }
-            order_tile<D, CB>();
+            float last = 0.f;                      // (added behind the next one's exponential, as in Stats)
+            tile_in_order<E, D, CB>(
+                tile, mm, g, [&](const x8& k, int kk, int cb, const f32x4& s) { return mfma(q[cb][kk], k, s); },
+                [&](int kb, int x, const f32x4 (&s)[CB]) {
+                  const float p = exp2_(fmaf(s[x >> 2][x & 3], a.c2, -ref[x >> 2][x & 3]));
+                  const int y = (x + 4 * CB - 1) % (4 * CB);
+                  float& of = sum[x > 0 ? kb : kb > 0 ? kb - 1 : 0];
+                  of = fmaf(last, inv[y >> 2][y & 3], of);
+                  last = p;
+                });
+            sum[3] = fmaf(last, inv[CB - 1][3], sum[3]);
           }
 #pragma unroll
           for (int kb = 0; kb < 4; ++kb) sum[kb] = column_sum(sum[kb]);
