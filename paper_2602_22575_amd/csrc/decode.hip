@@ -34,6 +34,7 @@ namespace {
 using namespace cache;
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kCus = 256;
 constexpr int kSplitWaves = 8;                  // of a workgroup without wide blocks, where the keys are split
 constexpr int kKeys = 32, kWideKeys = 64;       // tiles of the two walks
 constexpr int kNarrowRows = 16, kWideRows = 32 * kWaves;   // query rows of a workgroup
@@ -761,26 +762,38 @@ Shape shape_of(const DecodeArgs& a) {
   // Few keys: a workgroup takes a sequence through both caches and nothing has to be joined.
   s.direct = a.L == 0 || a.L + a.Lo <= 512;
   s.wide_o = rows_o > kNarrowRows;
-  s.wide_s = s.wide_o || (rows_s > kNarrowRows && !s.direct);
+  // Up to 32 shared rows are two narrow blocks: on 32K keys of 8 heads 36 us, a wide one 40, of whose wavefronts one has rows (64 rows: 52 and 43).
+  s.wide_s = s.wide_o || (rows_s > 2 * kNarrowRows && !s.direct);
   const int rows_wg_s = s.wide_s ? kWideRows : kNarrowRows, rows_wg_o = s.wide_o ? kWideRows : kNarrowRows;
   s.blocks_s = (int)((rows_s + rows_wg_s - 1) / rows_wg_s);
   s.blocks_o = (int)((rows_o + rows_wg_o - 1) / rows_wg_o);
   const int64_t units_s = heads * s.blocks_s, units_o = heads * a.B * s.blocks_o;
-  // Workgroups that are in flight together: two wide ones on each CU.  One of eight wavefronts where all blocks are narrow: 128 KB on their
-  // way are enough (one sequence on 32K keys 31.4 us, two such workgroups a CU 35.1, three of four wavefronts 38.0), and every part more has to be joined.
-  const int64_t slots = 256 * (s.wide_s ? 2 : 1);
-  if (s.direct && (a.L > 0 || units_o >= slots || a.Lo <= 512)) {
+  if (s.direct && (a.L > 0 || units_o >= kCus || a.Lo <= 512)) {
     s.splits_s = 0;
     s.splits_o = 1;
     return s;
   }
   s.direct = false;
-  // One round of workgroups with the same number of keys each, 128 at least.  Own keys count half where the shared ones are read for several
-  // row blocks and wait for the matrix cores, not for memory (64 sequences on 128K keys 182 us, else 188; 200 on 16K 126 and 149).
-  const int64_t keys = (units_s * a.L + units_o * a.Lo / (s.blocks_s > 1 ? 2 : 1)) / slots;
-  auto split = [&](int64_t len) { return (int)(len == 0 ? 0 : len / (keys > 128 ? keys : 128) > 1 ? len / (keys > 128 ? keys : 128) : 1); };
-  s.splits_s = split(a.L);
-  s.splits_o = split(a.Lo);
+  // One round of workgroups with the same number of keys each, 128 at least: every part more has to be written and joined.
+  const int64_t keys_s = units_s * a.L, keys_o = units_o * a.Lo;
+  auto split = [](int64_t len, int64_t keys) { return (int)(len == 0 ? 0 : len / (keys > 128 ? keys : 128) > 1 ? len / (keys > 128 ? keys : 128) : 1); };
+  if (!s.wide_s) {
+    // One of eight wavefronts a CU: 128 KB on their way are enough (one sequence on 32K keys 30.5 us, two such workgroups a CU 34.4, three of
+    // four wavefronts 33.1).
+    s.splits_s = split(a.L, (keys_s + keys_o) / kCus);
+    s.splits_o = split(a.Lo, (keys_s + keys_o) / kCus);
+    return s;
+  }
+  // Wide blocks: one a CU, and two only where several row blocks share keys, so that the matrix cores are what they wait for, and there are
+  // many of them (32 sequences on 16K keys 24 us, with two 33; 64 on 16K 32 and 38, on 128K 183 and 164).
+  const int64_t keys_w = keys_s + (s.wide_o ? keys_o : 0);
+  const bool two = (a.L ? s.blocks_s : s.blocks_o) > 1 && keys_w > kCus * 1536;
+  // Narrow own blocks beside them wait for memory alone: they take the room that is left beside one, and beside two count half (64 sequences
+  // on 128K keys and up to 1024 of their own 171 us, else 177; 200 on 16K and 800 116 and 137).
+  const int64_t beside = s.wide_o ? 0 : keys_o;
+  const int64_t keys = two ? (keys_w + beside / 2) / (2 * kCus) : keys_w / kCus;
+  s.splits_s = split(a.L, keys);
+  s.splits_o = split(a.Lo, two || s.wide_o ? keys : (keys_w + beside) / (2 * kCus));
   return s;
 }
 

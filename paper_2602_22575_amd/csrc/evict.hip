@@ -41,7 +41,7 @@ struct Places {
 };
 
 constexpr int kT = 1024, kWaves = kT / 64;
-constexpr int kOneGroup = 20 * kT;  // rows that select_kernel takes (8 heads of 16K rows 25 us, of 32K 42; by stretches 26 and 33)
+constexpr int kOneGroup = 20 * kT;  // rows that select_kernel takes (8 heads of 16K rows 24 us, of 24K 31; by stretches 25 and 28)
 constexpr int kBlock = 4 * kT;      // rows that a workgroup looks at at once, four in a row a thread
 constexpr int kStretches = 64;      // a head's rows are cut into, as far as a stretch has no more than kMostBlocks blocks
 constexpr int kMostBlocks = 15;     // (its counts have 16 bits)
