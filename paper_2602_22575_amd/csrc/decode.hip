@@ -20,8 +20,9 @@
 // about 256 rows a KV head, the matrix cores beyond.
 //
 // Measured, bf16, D 128, 32 query heads on 8: one sequence on 32K keys 26 us and 4 for the join, 5.2 TB/s; 32 sequences on 32K keys and up to
-// 512 of their own each 42 and 7; 64 on 128K and up to 1024 of their own 163 and 8, 0.77 PFLOP/s.  Of a launch 3 us pass until
-// the first keys are asked for (arguments, indices, the first pass through the code) and 3 while the parts' states are written.
+// 512 of their own each 38 and 6; 64 on 128K and up to 1024 of their own 143 to 170, by the clock that the power limit leaves, and 8: 0.76 to
+// 0.9 PFLOP/s.  Of a launch 3 us pass until the first keys are asked for (arguments, indices, the first pass through the code) and 3 while
+// the parts' states are written.
 #include <type_traits>
 
 #include "cache_tile.h"

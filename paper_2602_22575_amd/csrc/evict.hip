@@ -7,9 +7,9 @@
 //   count_kernel, collect_kernel, list_kernel    more rows, a workgroup per stretch of 4096 or more: count the keys' upper 11 bits; collect
 //                  the other 21 bits of the rows that share the last one's; settle them (every workgroup for itself, from LDS where they
 //                  fit) and list.  Nothing is added up by atomics in memory, so that nothing has to be cleared.  Three passes over the weights by
-//                  all of the chip, 5, 8 and 10 us for 8 heads of 128K rows (one workgroup a head: 102, the instructions of one CU).
-// gather_kernel copies the listed rows of K and V and their weights.  Bound: HBM bandwidth of the copy, 28 us for 134 MB, 4.8 TB/s.
-// select_kernel is bound by one CU's dependent passes: 20 us for 20K rows, of which reading and the first count take 4, the two other
+//                  all of the chip, 4, 7 and 10 us for 8 heads of 128K rows (one workgroup a head: 102, the instructions of one CU).
+// gather_kernel copies the listed rows of K and V and their weights.  Bound: HBM bandwidth of the copy, 26 to 29 us for 134 MB, 4.6 to 5.1 TB/s.
+// select_kernel is bound by one CU's dependent passes: 19 us for 20K rows, of which reading and the first count take 4, the two other
 // counts 6, listing 4.
 #include "cache_tile.h"
 #include "s2o_internal.h"

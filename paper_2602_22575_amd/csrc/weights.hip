@@ -12,8 +12,9 @@
 // Rows are counted r = (t * B + b) * G + g, so that what a key is seen by is one range of rows.
 //
 // Bound: a score costs 2 D FLOP on the matrix cores and an exponential, a multiply-add and an addition on the vector units, which take about as
-// long; the two overlap by half.  64 queries of 32 heads on 128K keys of 8 (69 GFLOP a pass): statistics 79 us, sums 86, 0.87 and 0.80
-// PFLOP/s; in the first the matrix cores work 43 % of the time, the vector units 63 %, one or the other 89 %.
+// long (17.2 and 16.6 clocks for 64 lanes' worth of one product) and overlap by half (25.5 together).  64 queries of 32 heads on 128K keys of 8
+// (69 GFLOP a pass): statistics 72 to 81 us, sums 80 to 92, by the clock that the power limit leaves: 0.75 to 0.96 PFLOP/s.  All 8192 queries of a
+// prompt (275 GFLOP a pass): 260 and 340.
 //
 // Statistics are kept as a base-2 reference m and 1/l instead of one lse: rounding m + log2 l would cost the weights
 // 2^-20 of their value.  An lse that is given is turned into the same pair, its base-2 form rounded and the rest in the factor.
