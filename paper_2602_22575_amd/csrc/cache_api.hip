@@ -169,7 +169,8 @@ int check_scratch(const void* scratch, size_t bytes, size_t need) {
   return !scratch || misaligned(scratch, 256) || bytes < need ? S2O_ESCRATCH : S2O_OK;
 }
 
-int done(hipError_t e) { return e == hipSuccess ? S2O_OK : s2o::hip_fail(e); }
+// (Not supported: sizes whose launch would not fit, found before anything was launched.)
+int done(hipError_t e) { return e == hipSuccess ? S2O_OK : e == hipErrorNotSupported ? S2O_EUNSUPPORTED : s2o::hip_fail(e); }
 
 }  // namespace
 

@@ -803,7 +803,10 @@ hipError_t launch(DecodeArgs a, const Shape& s, hipStream_t stream) {
   const int64_t all_rows = (int64_t)a.Z * a.B * a.H * a.T;
   const int64_t units_s = (int64_t)a.Z * a.Hkv * s.splits_s, units_o = (int64_t)a.Z * a.Hkv * a.B * s.splits_o;
   const int64_t ids_s = (units_s + 7) / 8 * 8 * s.blocks_s, ids_o = (units_o + 7) / 8 * 8 * s.blocks_o;
-  if (ids_s + ids_o <= 0 || ids_s + ids_o > 0x7fffffff) return hipErrorInvalidValue;
+  int lanes = 1;
+  while (lanes < 1024 / D && lanes * 2 <= s.parts()) lanes *= 2;
+  const int64_t per = 256 / (D / 4 * lanes), joins = (all_rows + per - 1) / per;
+  if (!fits_launch(ids_s + ids_o, 64 * kSplitWaves) || (s.parts() > 1 && !fits_launch(joins, 256))) return hipErrorNotSupported;
   a.rows = all_rows;
   a.units_s = (int)units_s; a.units_o = (int)units_o; a.ids_s = (int)ids_s;
   a.by_blocks_s = Divisor(8 * s.blocks_s); a.by_blocks_o = Divisor(8 * s.blocks_o);
@@ -818,10 +821,7 @@ hipError_t launch(DecodeArgs a, const Shape& s, hipStream_t stream) {
   else hipLaunchKernelGGL((decode_kernel<E, D, false, false, kSplitWaves>), grid, dim3(64 * kSplitWaves), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.part_acc) return e;
-  int lanes = 1;
-  while (lanes < 1024 / D && lanes * 2 <= s.parts()) lanes *= 2;
-  const int64_t per = 256 / (D / 4 * lanes);
-  hipLaunchKernelGGL((decode_join_kernel<E, D>), dim3((unsigned)((all_rows + per - 1) / per)), dim3(256), 0, stream, a, s.parts(), lanes);
+  hipLaunchKernelGGL((decode_join_kernel<E, D>), dim3((unsigned)joins), dim3(256), 0, stream, a, s.parts(), lanes);
   return hipGetLastError();
 }
 

@@ -424,29 +424,27 @@ size_t evict_scratch_bytes(const EvictArgs& a) {
 }
 
 hipError_t launch_evict(EvictArgs a, void* scratch, hipStream_t stream) {
-  const int64_t heads = (int64_t)a.Z * a.Hkv;
-  if (heads > 0x7fffffff) return hipErrorInvalidValue;
-  if (a.L <= kOneGroup) {
-    const dim3 grid((unsigned)heads);
-    if (a.L <= 4 * kT) hipLaunchKernelGGL(select_kernel<4 * kT>, grid, dim3(kT), 0, stream, a);
-    else hipLaunchKernelGGL(select_kernel<kOneGroup>, grid, dim3(kT), 0, stream, a);
+  const int64_t heads = (int64_t)a.Z * a.Hkv, blocks = a.L <= kOneGroup ? heads : heads * stretches(a.L);
+  constexpr int kEach = 4;
+  const int rows = 2048 / a.D * kEach, chunks = (a.keep + rows - 1) / rows;
+  const bool moves = a.K || a.V || a.weights_out;
+  if (!fits_launch(blocks, kT) || (moves && !fits_launch(heads * chunks, 256))) return hipErrorNotSupported;
+  const dim3 grid((unsigned)blocks);
+  if (a.L <= 4 * kT) {
+    hipLaunchKernelGGL(select_kernel<4 * kT>, grid, dim3(kT), 0, stream, a);
+  } else if (a.L <= kOneGroup) {
+    hipLaunchKernelGGL(select_kernel<kOneGroup>, grid, dim3(kT), 0, stream, a);
   } else {
     a.scratch = static_cast<uint32_t*>(scratch);
-    const int64_t blocks = heads * stretches(a.L);
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks);
     hipLaunchKernelGGL(count_kernel, grid, dim3(kT), 0, stream, a);
     hipLaunchKernelGGL(collect_kernel, grid, dim3(kT), 0, stream, a);
     hipLaunchKernelGGL(list_kernel, grid, dim3(kT), 0, stream, a);
   }
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || (!a.K && !a.V && !a.weights_out)) return e;
-  constexpr int kEach = 4;
-  const int rows = 2048 / a.D * kEach, chunks = (a.keep + rows - 1) / rows;
-  if (heads * chunks > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)(heads * chunks), a.V ? 2 : 1);
-  if (a.D == 128) hipLaunchKernelGGL((gather_kernel<128, kEach>), grid, dim3(256), 0, stream, a, chunks);
-  else hipLaunchKernelGGL((gather_kernel<64, kEach>), grid, dim3(256), 0, stream, a, chunks);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !moves) return e;
+  const dim3 gather((unsigned)(heads * chunks), a.V ? 2 : 1);
+  if (a.D == 128) hipLaunchKernelGGL((gather_kernel<128, kEach>), gather, dim3(256), 0, stream, a, chunks);
+  else hipLaunchKernelGGL((gather_kernel<64, kEach>), gather, dim3(256), 0, stream, a, chunks);
   return hipGetLastError();
 }
 

@@ -96,6 +96,9 @@ hipError_t launch_prefix(const AttnArgs& a, hipStream_t stream);
 // Notes a failed HIP call for s2o_last_hip_error; S2O_EHIP.
 int hip_fail(hipError_t e);
 
+// A launch counts its threads in 32 bits.  (The cache's launches return hipErrorNotSupported, before the first one, where that is too few.)
+inline bool fits_launch(int64_t blocks, int threads) { return blocks > 0 && blocks <= (int64_t)0xffffffff / threads; }
+
 // Quotient and rest of non-negative numbers below 2^31 by d = 1 .. 2^31 - 1 that the host has prepared: a product's upper half instead of the
 // forty instructions of a division.  mul = ceil(2^(31 + s) / d), 2^(s-1) < d <= 2^s: n * mul / 2^(31 + s) is off by less than 1/d above.
 // Laid out to be loaded in one piece.

@@ -501,16 +501,15 @@ hipError_t launch(WeightsArgs a, hipStream_t stream) {
   a.by_Z = Divisor(a.Z); a.by_Hkv = Divisor(a.Hkv); a.by_G = Divisor(a.G); a.by_BG = Divisor(a.B * a.G);
   a.by_key_parts = Divisor(a.key_parts); a.by_row_parts = Divisor(a.row_parts);
   const int64_t heads = (int64_t)a.Z * a.Hkv, rows = heads * a.B * a.T * a.G;
-  const int64_t sum_blocks = heads * a.row_parts * a.ranges;
-  if (sum_blocks > 0x7fffffff) return hipErrorInvalidValue;
+  const int64_t sum_blocks = heads * a.row_parts * a.ranges, blocks = heads * a.row_blocks * a.key_parts, joins = (rows + 15) / 16;
+  if (!fits_launch(sum_blocks, kThreads)) return hipErrorNotSupported;
+  if (!a.lse && (!fits_launch(blocks, kThreads) || (a.key_parts > kFewParts && !fits_launch(joins, 256)))) return hipErrorNotSupported;
   if (a.lse) {
     hipLaunchKernelGGL((sum_kernel<E, D, CB, true>), dim3((unsigned)sum_blocks), dim3(kThreads), 0, stream, a);
   } else {
-    const int64_t blocks = heads * a.row_blocks * a.key_parts;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     hipLaunchKernelGGL((stats_kernel<E, D, CB>), dim3((unsigned)blocks), dim3(kThreads), 0, stream, a);
     if (a.key_parts > kFewParts)
-      hipLaunchKernelGGL(stats_join_kernel, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, a.stats, rows, a.key_parts);
+      hipLaunchKernelGGL(stats_join_kernel, dim3((unsigned)joins), dim3(256), 0, stream, a.stats, rows, a.key_parts);
     hipLaunchKernelGGL((sum_kernel<E, D, CB, false>), dim3((unsigned)sum_blocks), dim3(kThreads), 0, stream, a);
   }
   if (a.row_parts > 1)

@@ -248,3 +248,16 @@ def test_evict_refuses_scratch_on_top_of_an_output(lib):
     need = b.s2o_evict_sizes(p)["scratch"]
     args = at[:4] + [C.byref(p)] + at[4:9] + [at[9], need, None]
     _refused(lib.s2o_evict, args, [(10, x, b.S2O_EINVAL) for x in at[:9]])
+
+
+def test_launches_that_do_not_fit_are_refused(lib):
+    at = [C.c_void_p((i + 1) << 46) for i in range(10)]
+    p = b.make_decode_params(1, 1 << 24, 4, 4, 128, 1, 96, 24)
+    assert lib.s2o_decode(*at[:7], C.byref(p), at[7], at[8], None, 0, None) == b.S2O_EUNSUPPORTED
+    p = b.make_decode_params(1 << 22, 64, 4, 4, 64, 1, 1000)
+    assert lib.s2o_decode(*at[:3], None, None, None, None, C.byref(p), at[7], at[8], at[9], 1 << 62, None) == b.S2O_EUNSUPPORTED
+    p = b.make_weights_params(1 << 23, 1, 2, 2, 64, 1, 70)
+    assert lib.s2o_key_weights(at[0], at[1], at[2], None, C.byref(p), None, at[3], None, 0, None) == b.S2O_EUNSUPPORTED
+    assert lib.s2o_key_weights(at[0], at[1], None, None, C.byref(p), None, at[3], at[4], 1 << 62, None) == b.S2O_EUNSUPPORTED
+    p = b.make_evict_params(1 << 23, 2, 64, 100, 10)
+    assert lib.s2o_evict(at[0], at[1], at[2], None, C.byref(p), at[3], at[4], None, at[5], None, None, 0, None) == b.S2O_EUNSUPPORTED
