@@ -16,7 +16,6 @@ namespace s2o {
 namespace cache {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
@@ -114,7 +113,7 @@ __device__ __forceinline__ const A& kernel_args() {
   return *(const A*)p;
 }
 
-constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 
 // rows in a cache: what the caller says, kept inside the memory it has
 __device__ __forceinline__ int filled(const int32_t* lens, int i, int most) {

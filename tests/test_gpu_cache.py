@@ -94,6 +94,9 @@ DECODE = [
     (1, 17, 40, 8, 128, 1, 600, 5, "f16", False, [0], None),
     (5, 7, 2, 1, 64, 2, 513, 3, "bf16", True, [513, 0, 1, 64, 65], None),
     (1, 64, 32, 8, 128, 1, 2500, 30, "bf16", False, None, None),
+    (1, 5, 8, 2, 128, 1, 3000, 40, "bf16", False, None, None),                # 20 rows on a KV head
+    (2, 2, 16, 4, 64, 3, 2000, 33, "f16", True, [2000, 31], [[33, 2], [0, 33]]),   # 24
+    (1, 8, 4, 1, 64, 1, 1200, 0, "bf16", False, [1187], None),                # 32
 ]
 
 
