@@ -487,11 +487,25 @@ def _call(fn, ctx, *args):
         _check(fn(*args))
 
 
-def _scratch_for(scratch, size, dev, fresh):
+def _allocate(stream, dev, allocate):
+    """allocate() -> tensors for kernels on `stream`, of memory that is free there: what torch's current stream has freed may still
+    be in use by it.  The caller may go on with them on the current stream (once that has waited)."""
+    import torch
+    if stream is None:
+        return allocate()
+    with torch.cuda.stream(stream):
+        tensors = allocate()
+    current = torch.cuda.current_stream(dev)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(current)
+    return tensors
+
+
+def _scratch_for(scratch, size, dev, stream):
     import torch
     if scratch is None and size:
-        scratch = torch.empty(size, dtype=torch.uint8, device=dev)
-        fresh.append(scratch)
+        scratch, = _allocate(stream, dev, lambda: (torch.empty(size, dtype=torch.uint8, device=dev),))
     if scratch is not None and (scratch.device != dev or not scratch.is_contiguous()):
         raise ValueError(f"scratch: expected a contiguous tensor on {dev}")
     return scratch, 0 if scratch is None else scratch.numel() * scratch.element_size()
@@ -514,22 +528,24 @@ def s2o_decode(Q, K, V, params: S2ODecodeParams, own_K=None, own_V=None, lens=No
     for name, t, kind, shape in (("lens", lens, torch.int32, rows[:1]), ("own_lens", own_lens, torch.int32, rows[:2]), ("lse", lse, torch.float32, rows)):
         if t is not None:
             _check_layout(name, t, kind, dev, shape)
-    fresh = []
-    if O is None:
-        shape, strides = layout["O"]
-        if strides is None and layout["Q"][1] is None:
-            O = torch.empty_like(Q)                      # (packed like it; quicker)
-        elif strides is None:
-            O = torch.empty(shape, dtype=dtype, device=dev)
-        else:
-            O = torch.empty_strided(shape, strides + (1,), dtype=dtype, device=dev)
-        fresh.append(O)
-    if lse is None and want_lse:
-        lse = torch.empty(rows, dtype=torch.float32, device=dev)
-        fresh.append(lse)
-    scratch, size = _scratch_for(scratch, size, dev, fresh)
-    _keep_alive_on(stream, *fresh)
     handle, ctx = _on_device(dev, stream)
+
+    def allocate():
+        new, new_lse = O, lse
+        if new is None:
+            shape, strides = layout["O"]
+            if strides is None and layout["Q"][1] is None:
+                new = torch.empty_like(Q)                # (packed like it; quicker)
+            elif strides is None:
+                new = torch.empty(shape, dtype=dtype, device=dev)
+            else:
+                new = torch.empty_strided(shape, strides + (1,), dtype=dtype, device=dev)
+        if new_lse is None and want_lse:
+            new_lse = torch.empty(rows, dtype=torch.float32, device=dev)
+        return new, new_lse
+
+    O, lse = _allocate(stream, dev, allocate)
+    scratch, size = _scratch_for(scratch, size, dev, stream)
     _call(lib.s2o_decode, ctx, Q.data_ptr(), _ptr(K), _ptr(V), _ptr(own_K), _ptr(own_V), _ptr(lens), _ptr(own_lens), C.byref(params),
           O.data_ptr(), _ptr(lse), _ptr(scratch), size, handle)
     return O, lse
@@ -551,19 +567,10 @@ def s2o_key_weights(Q, K, params: S2OWeightsParams, lse=None, lens=None, prev=No
                              ("out", out, torch.float32, shape)):
         if t is not None:
             _check_layout(name, t, kind, dev, s)
-    fresh = []
     handle, ctx = _on_device(dev, stream)
     if out is None:
-        if lens is None:
-            out = torch.empty(shape, dtype=torch.float32, device=dev)
-        elif stream is None:
-            out = torch.zeros(shape, dtype=torch.float32, device=dev)
-        else:
-            with torch.cuda.stream(stream):      # cleared where the kernels will run
-                out = torch.zeros(shape, dtype=torch.float32, device=dev)
-        fresh.append(out)
-    scratch, size = _scratch_for(scratch, size, dev, fresh)
-    _keep_alive_on(stream, *fresh)
+        out, = _allocate(stream, dev, lambda: ((torch.empty if lens is None else torch.zeros)(shape, dtype=torch.float32, device=dev),))
+    scratch, size = _scratch_for(scratch, size, dev, stream)
     _call(lib.s2o_key_weights, ctx, Q.data_ptr(), K.data_ptr(), _ptr(lse), _ptr(lens), C.byref(params), _ptr(prev), out.data_ptr(),
           _ptr(scratch), size, handle)
     return out
@@ -600,22 +607,22 @@ def s2o_evict(K, V, weights, params: S2OEvictParams, lens=None, out_K=None, out_
                              ("kept", kept, torch.int32, left), ("out_lens", out_lens, torch.int32, rows[:1])):
         if t is not None:
             _check_layout(name, t, kind, dev, s)
-    fresh = []
+    handle, ctx = _on_device(dev, stream)
 
     def new(t, shape, kind, strides=None):
-        if t is None:
-            t = torch.empty(shape, dtype=kind, device=dev) if strides is None else torch.empty_strided(shape, strides + (1,), dtype=kind, device=dev)
-            fresh.append(t)
-        return t
+        if t is not None:
+            return t
+        return torch.empty(shape, dtype=kind, device=dev) if strides is None else torch.empty_strided(shape, strides + (1,), dtype=kind, device=dev)
 
-    if K is not None:
-        (shape, ks), (_, vs) = layout["out_K"], layout["out_V"]
-        out_K, out_V = new(out_K, shape, dtype, ks), new(out_V, shape, dtype, vs)
-    out_weights, kept = new(out_weights, left, torch.float32), new(kept, left, torch.int32)
-    out_lens = new(out_lens, rows[:1], torch.int32)
-    scratch, size = _scratch_for(scratch, size, dev, fresh)
-    _keep_alive_on(stream, *fresh)
-    handle, ctx = _on_device(dev, stream)
+    def allocate():
+        k = v = None
+        if K is not None:
+            (moved, ks), (_, vs) = layout["out_K"], layout["out_V"]
+            k, v = new(out_K, moved, dtype, ks), new(out_V, moved, dtype, vs)
+        return k, v, new(out_weights, left, torch.float32), new(kept, left, torch.int32), new(out_lens, rows[:1], torch.int32)
+
+    out_K, out_V, out_weights, kept, out_lens = _allocate(stream, dev, allocate)
+    scratch, size = _scratch_for(scratch, size, dev, stream)
     _call(lib.s2o_evict, ctx, _ptr(K), _ptr(V), weights.data_ptr(), _ptr(lens), C.byref(params), _ptr(out_K), _ptr(out_V), out_weights.data_ptr(),
           kept.data_ptr(), out_lens.data_ptr(), _ptr(scratch), size, handle)
     return Evicted(out_K, out_V, out_weights, kept, out_lens)

@@ -540,6 +540,32 @@ def test_another_stream():
     assert _same(a, b) and (w[..., 1999:] == 0).all()
 
 
+def test_outputs_for_another_stream_do_not_take_over_memory_that_is_in_use():
+    """Memory that the current stream has freed, but not passed, is not what a call on another stream writes to."""
+    t, p = make_decode(1, 64, 32, 8, 128, 1, 600, 0, "bf16")
+    w = torch.rand(1, 8, 600, device="cuda:0")
+    pw, pe = s2o.make_weights_params(1, 64, 32, 8, 128, 1, 600), s2o.make_evict_params(1, 8, 128, 600, 100, 2, 2)
+
+    def calls(stream):
+        O, lse = s2o.s2o_decode(t[0], t[1], t[2], p, stream=stream)
+        e = s2o.s2o_evict(t[1], t[2], w, pe, stream=stream)
+        return [O, lse, s2o.s2o_key_weights(t[0], t[1], pw, stream=stream), e.K, e.V, e.weights, e.kept, e.lens]
+
+    want = calls(None)
+    a = torch.zeros(4096, 4096, dtype=torch.bfloat16, device="cuda:0")
+    late = [torch.empty_like(x) for x in want]
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(200):
+        torch.mm(a, a)                                     # tens of milliseconds, and behind them:
+    for x in late:
+        x.fill_(7)
+    del late, x
+    got = calls(s)
+    torch.cuda.synchronize()
+    assert _same(got, want)
+
+
 def test_two_streams_at_once():
     """Calls with buffers and workspaces of their own, on two streams together."""
     sides = [_three(seed) for seed in (3, 4)]
