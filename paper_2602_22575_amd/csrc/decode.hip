@@ -61,10 +61,11 @@ struct Walk {
   f32x4 o[CB][D / 16];
   float m[CB], l[CB];            // reference (base 2) and the lane's part of the sum
 
-  __device__ __forceinline__ void start() {
+  // keep: the references stay
+  __device__ __forceinline__ void start(bool keep = false) {
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
-      m[cb] = -INFINITY;
+      if (!keep) m[cb] = -INFINITY;
       l[cb] = 0.f;
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) o[cb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -238,10 +239,11 @@ struct Walk {
   // Tiles from .. to - 1 of 64 keys, by all four wavefronts together; `rows` as above.  ka, kb_, va, vb: K and V tile of even and odd steps (separate
   // arrays, so that the compiler sees that reads of one need not wait for the loads that fill another).
   //
-  // The first 16 keys find the references, the last tiles may have hidden keys.  For the others, if `fast`, a tile's products and exponentials
-  // are one straight run of instructions, its second half's exponentials behind its first half's products: numerators are formed
-  // against the references as they are, and a reference moves afterwards, where two tiles' sum has outgrown 2^10.  Returns false where a numerator
-  // or an accumulator may have outgrown its type on the way: all of it is to be done again, not fast.
+  // The first keys find the references that there are not yet (16 of them; 64 for fp16, whose numerators have room for 2^15), the last tiles may have
+  // hidden keys.  For the others, if `fast`, a tile's products and exponentials are one straight run of instructions, its second half's
+  // exponentials behind its first half's products: numerators are formed against the references as they are, and a reference moves
+  // afterwards, where two tiles' sum has outgrown 2^10.  Returns false where a numerator or an accumulator may have outgrown its type on the
+  // way: all of it is to be done again, with the references that are known by then.
   template <class F>
   __device__ __forceinline__ bool wide(const E* K, const E* V, int64_t kstride, int64_t vstride, int len, int from, int to, float c2,
                                        unsigned char* ka, unsigned char* kb_, unsigned char* va, unsigned char* vb, int wave, int lane,
@@ -379,7 +381,7 @@ struct Walk {
       for (int cb = 0; cb < CB; ++cb) {
         const float most = column_max(sum[cb]);
         fits &= !(__builtin_amdgcn_ballot_w64(!(sum[cb] <= kMost)) != 0);
-        const int up = most > kMove && most <= kMost ? __builtin_amdgcn_frexp_expf(most) : 0;
+        const int up = most > kMove && most < INFINITY ? __builtin_amdgcn_frexp_expf(most) : 0;
         const float alpha = __builtin_amdgcn_ldexpf(1.0f, -up);
         m[cb] += (float)up;
         l[cb] *= alpha;
@@ -397,11 +399,16 @@ struct Walk {
     if (t < full) {
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
-        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+        float top = -INFINITY;
 #pragma unroll
-        for (int kk = 0; kk < D / 32; ++kk) s = mfma(*reinterpret_cast<const x8*>(ka + (at<D>(mm, g) ^ (kk << 6))), q[cb][kk], s);
-        const float top = column_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))) * c2;
-        const float first = m[cb] == -INFINITY ? top : m[cb];   // (a second cache goes on with the first one's)
+        for (int kb = 0; kb < (__is_same(E, __bf16) ? 1 : 4); ++kb) {
+          f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int kk = 0; kk < D / 32; ++kk) s = mfma(*reinterpret_cast<const x8*>(ka + 16 * kb * 2 * D + (at<D>(mm, g) ^ (kk << 6))), q[cb][kk], s);
+          top = fmaxf(top, fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])));
+        }
+        top = column_max(top) * c2;
+        const float first = m[cb] == -INFINITY ? top : m[cb];   // (a second cache goes on with the first one's, a second attempt with those that the first found)
         m[cb] = first;
         fits &= __builtin_amdgcn_ballot_w64(!(fabsf(first) < INFINITY)) == 0;
       }
@@ -598,19 +605,19 @@ __device__ __forceinline__ void wide_block(const Block<E, D>& k, unsigned char* 
   int t_of[2];
   bool loaded = false;
 #pragma unroll 1
-  for (int fast = 1; fast >= 0; --fast) {
-    w.start();
+  for (int attempt = 0;; ++attempt) {                      // fast, fast with the references that the first attempt found, not fast
+    w.start(attempt == 1);
     bool fits = true;
 #pragma unroll 1
     for (int own = k.first_cache(); own < (k.shared ? 1 : 2); ++own) {
       const auto c = k.cache(own, kWideKeys);
-      fits &= w.wide(c.K, c.V, c.kst, c.vst, c.len, c.from, c.to, c.c2, ka, kb, va, vb, wave, lane, fast, [&](int (&lim)[2], int& lim_all) {
+      fits &= w.wide(c.K, c.V, c.kst, c.vst, c.len, c.from, c.to, c.c2, ka, kb, va, vb, wave, lane, attempt < 2, [&](int (&lim)[2], int& lim_all) {
         if (!loaded) k.load(w, r0, t_of, lane);
         loaded = true;
         k.limits(c, own, kWideRows, t_of, lim, lim_all);
       });
     }
-    if (!fast || !__syncthreads_or(!fits)) break;
+    if (attempt == 2 || !__syncthreads_or(!fits)) break;
   }
   // O^T to rows: lane l's piece of row l % 16 is dims 16 * db + 4 * g .. + 3
 #pragma unroll
