@@ -9,8 +9,8 @@
 //                  fit) and list.  Nothing is added up by atomics in memory, so that nothing has to be cleared.  Three passes over the weights by
 //                  all of the chip, 4, 7 and 10 us for 8 heads of 128K rows (one workgroup a head: 102, the instructions of one CU).
 // gather_kernel copies the listed rows of K and V and their weights.  Bound: HBM bandwidth of the copy, 26 to 29 us for 134 MB, 4.6 to 5.1 TB/s.
-// select_kernel is bound by one CU's dependent passes: 19 us for 20K rows, of which reading and the first count take 4, the two other
-// counts 6, listing 4.
+// select_kernel is bound by one CU's dependent passes: 17 us for 20K rows, of which reading and the first count take 4, the two other
+// counts 5, listing 3.
 #include "cache_tile.h"
 #include "s2o_internal.h"
 
@@ -41,7 +41,7 @@ struct Places {
 };
 
 constexpr int kT = 1024, kWaves = kT / 64;
-constexpr int kOneGroup = 20 * kT;  // rows that select_kernel takes (8 heads of 16K rows 24 us, of 24K 31; by stretches 25 and 28)
+constexpr int kOneGroup = 20 * kT;  // rows that select_kernel takes (8 heads of 16K rows 22 us, of 24K 29; by stretches 24 and 27)
 constexpr int kBlock = 4 * kT;      // rows that a workgroup looks at at once, four in a row a thread
 constexpr int kStretches = 64;      // a head's rows are cut into, as far as a stretch has no more than kMostBlocks blocks
 constexpr int kMostBlocks = 15;     // (its counts have 16 bits)
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(kT) void list_kernel(const EvictArgs a) {
   }
 }
 
-// kRows: of a head at most.
+// kRows: of a head at most; a thread holds its share of them in registers (8 heads of 12K rows 18 us, in the form for 20K 20).
 template <int kRows>
 __global__ __launch_bounds__(kT) void select_kernel(const EvictArgs a) {
   touch_args<EvictArgs>();
@@ -336,8 +336,17 @@ __global__ __launch_bounds__(kT) void select_kernel(const EvictArgs a) {
       }
   }
   __syncthreads();
-  // From here on a thread has a stretch of its own: an odd number of pieces of four rows, so that a wavefront's reads meet different banks.
+  // From here on a thread has a stretch of its own, in registers: an odd number of pieces of four rows, so that a wavefront's reads meet different banks.
+  constexpr int kPieces = (kRows / kBlock) | 1;
   const int per = 4 * (((p.n + kBlock - 1) / kBlock) | 1), from = min(tid * per, p.n), to = min(from + per, p.n);
+  u32x4 mine[kPieces];
+#pragma unroll
+  for (int j = 0; j < kPieces; ++j) {
+    mine[j] = *reinterpret_cast<const u32x4*>(keys + min(tid * per + 4 * j, kRows - 4));
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (from + 4 * j + e >= to) mine[j][e] = 0;
+  }
   uint32_t key = 0, known = 0;                             // what is known of the last row's key, from the top down
   int ties = p.want;                                       // places for the rows that share it
   if (choose) {
@@ -347,13 +356,11 @@ __global__ __launch_bounds__(kT) void select_kernel(const EvictArgs a) {
       if (shift != 21) {
         for (int i = tid; i < kBins; i += kT) counts[i] = 0;
         __syncthreads();
-#pragma unroll 1
-        for (int i = from; i < to; i += 4) {
-          const u32x4 k = *reinterpret_cast<const u32x4*>(keys + i);
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (i + e < to && k[e] && (k[e] & known) == key) atomicAdd(&counts[(k[e] >> shift) & mask], 1u);
-        }
+            if (mine[j][e] && (mine[j][e] & known) == key) atomicAdd(&counts[(mine[j][e] >> shift) & mask], 1u);
         __syncthreads();
       }
       const Bin last = find_bin(counts, part, &found, ties, tid);
@@ -364,20 +371,17 @@ __global__ __launch_bounds__(kT) void select_kernel(const EvictArgs a) {
       __syncthreads();
     }
   }
-  static_assert(4 * ((kRows / kBlock) | 1) <= 64, "a thread's rows are the bits of a word");
+  static_assert(4 * kPieces <= 64, "a thread's rows are the bits of a word");
   uint64_t sure = 0, tie = 0;
-#pragma unroll 1
-  for (int i = from; i < to; i += 4) {
-    const u32x4 k = *reinterpret_cast<const u32x4*>(keys + i);
-    uint32_t s4 = 0, t4 = 0;
+#pragma unroll
+  for (int j = 0; j < kPieces; ++j)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (i + e < to && (k[e] == 0 || all || (choose && (k[e] & known) > key))) s4 |= 1u << e;
-      if (i + e < to && k[e] != 0 && choose && (k[e] & known) == key) t4 |= 1u << e;
+      const uint32_t k = mine[j][e];
+      sure |= (uint64_t)(k == 0 || all || (choose && (k & known) > key)) << (4 * j + e);
+      tie |= (uint64_t)(k != 0 && choose && (k & known) == key) << (4 * j + e);
     }
-    sure |= (uint64_t)s4 << (i - from);
-    tie |= (uint64_t)t4 << (i - from);
-  }
+  sure &= to - from < 64 ? (1ull << (to - from)) - 1 : ~0ull;
   const Sums sums = block_scan(__popcll(sure), __popcll(tie), part, tid);
   list_rows(a.kept + head * a.keep, from, sure, tie, sums.a, sums.b, ties);
 }
@@ -432,6 +436,8 @@ hipError_t launch_evict(EvictArgs a, void* scratch, hipStream_t stream) {
   const dim3 grid((unsigned)blocks);
   if (a.L <= 4 * kT) {
     hipLaunchKernelGGL(select_kernel<4 * kT>, grid, dim3(kT), 0, stream, a);
+  } else if (a.L <= 12 * kT) {
+    hipLaunchKernelGGL(select_kernel<12 * kT>, grid, dim3(kT), 0, stream, a);
   } else if (a.L <= kOneGroup) {
     hipLaunchKernelGGL(select_kernel<kOneGroup>, grid, dim3(kT), 0, stream, a);
   } else {
