@@ -769,7 +769,9 @@ Shape shape_of(const DecodeArgs& a) {
   const int64_t rows_o = (int64_t)a.T * a.G, rows_s = a.B * rows_o, heads = (int64_t)a.Z * a.Hkv;
   // Few keys: a workgroup takes a sequence through both caches and nothing has to be joined.
   s.direct = a.L == 0 || a.L + a.Lo <= 512;
-  s.wide_o = rows_o > kNarrowRows;
+  // A sequence's rows are up to three narrow blocks (20 rows on 976 + 13 keys of 45 x 5 sequences 75 us, a wide block 93; 35 on 602 + 43 of 55 x 3 82 and
+  // 105; 64 on 4096 46 and 43), two where nothing is joined (35 on 235 keys 81 and 67).
+  s.wide_o = rows_o > (s.direct ? 2 : 3) * kNarrowRows;
   // Up to 32 shared rows are two narrow blocks: on 32K keys of 8 heads 36 us, a wide one 40, of whose wavefronts one has rows (64 rows: 52 and 43).
   s.wide_s = s.wide_o || (rows_s > 2 * kNarrowRows && !s.direct);
   const int rows_wg_s = s.wide_s ? kWideRows : kNarrowRows, rows_wg_o = s.wide_o ? kWideRows : kNarrowRows;

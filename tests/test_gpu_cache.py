@@ -97,6 +97,11 @@ DECODE = [
     (1, 5, 8, 2, 128, 1, 3000, 40, "bf16", False, None, None),                # 20 rows on a KV head
     (2, 2, 16, 4, 64, 3, 2000, 33, "f16", True, [2000, 31], [[33, 2], [0, 33]]),   # 24
     (1, 8, 4, 1, 64, 1, 1200, 0, "bf16", False, [1187], None),                # 32
+    (1, 5, 8, 2, 128, 5, 700, 90, "bf16", False, None, [[90, 4, 5, 6, 0]]),   # 20 rows a sequence
+    (2, 3, 10, 2, 64, 7, 900, 300, "f16", True, [900, 17], [[300, 7, 2], [31, 32, 33]]),   # 35
+    (1, 4, 8, 2, 128, 12, 2000, 700, "bf16", False, None, [[700, 13, 64, 1]]),   # 48
+    (1, 4, 5, 1, 128, 7, 0, 260, "bf16", False, None, [[260, 3, 0, 100]]),
+    (1, 4, 8, 2, 64, 8, 40, 30, "f16", False, [39], [[30, 8, 1, 0]]),         # 32, nothing joined
 ]
 
 
