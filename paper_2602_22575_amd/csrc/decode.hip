@@ -767,8 +767,10 @@ struct Shape {
 Shape shape_of(const DecodeArgs& a) {
   Shape s{};
   const int64_t rows_o = (int64_t)a.T * a.G, rows_s = a.B * rows_o, heads = (int64_t)a.Z * a.Hkv;
-  // Few keys: a workgroup takes a sequence through both caches and nothing has to be joined.
-  s.direct = a.L == 0 || a.L + a.Lo <= 512;
+  // Few keys: a workgroup takes a sequence through both caches and nothing has to be joined.  Not where many sequences, more than there is room
+  // for at once, would read the same keys (35 sequences on each of 5 caches of 444 keys 55 us, so 79; 64 caches of 4 sequences 58 and 47).
+  const bool many = heads * a.B > 2 * kCus && rows_s > 2 * kNarrowRows && a.L > 64;
+  s.direct = a.L == 0 || (a.L + a.Lo <= 512 && !many);
   // A sequence's rows are up to three narrow blocks (20 rows on 976 + 13 keys of 45 x 5 sequences 75 us, a wide block 93; 35 on 602 + 43 of 55 x 3 82 and
   // 105; 64 on 4096 46 and 43), two where nothing is joined (35 on 235 keys 81 and 67).
   s.wide_o = rows_o > (s.direct ? 2 : 3) * kNarrowRows;

@@ -253,7 +253,7 @@ def test_evict_refuses_scratch_on_top_of_an_output(lib):
 def test_launches_that_do_not_fit_are_refused(lib):
     at = [C.c_void_p((i + 1) << 46) for i in range(10)]
     p = b.make_decode_params(1, 1 << 24, 4, 4, 128, 1, 96, 24)
-    assert lib.s2o_decode(*at[:7], C.byref(p), at[7], at[8], None, 0, None) == b.S2O_EUNSUPPORTED
+    assert lib.s2o_decode(*at[:7], C.byref(p), at[7], at[8], at[9], 1 << 62, None) == b.S2O_EUNSUPPORTED
     p = b.make_decode_params(1 << 22, 64, 4, 4, 64, 1, 1000)
     assert lib.s2o_decode(*at[:3], None, None, None, None, C.byref(p), at[7], at[8], at[9], 1 << 62, None) == b.S2O_EUNSUPPORTED
     p = b.make_weights_params(1 << 23, 1, 2, 2, 64, 1, 70)

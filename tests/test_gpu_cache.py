@@ -102,6 +102,8 @@ DECODE = [
     (1, 4, 8, 2, 128, 12, 2000, 700, "bf16", False, None, [[700, 13, 64, 1]]),   # 48
     (1, 4, 5, 1, 128, 7, 0, 260, "bf16", False, None, [[260, 3, 0, 100]]),
     (1, 4, 8, 2, 64, 8, 40, 30, "f16", False, [39], [[30, 8, 1, 0]]),         # 32, nothing joined
+    (2, 70, 8, 4, 64, 1, 90, 11, "bf16", False, [90, 33], [list(range(12)) * 5 + [11] * 10] * 2),   # few keys of many sequences
+    (1, 140, 4, 4, 128, 2, 300, 0, "f16", True, [299], None),
 ]
 
 
